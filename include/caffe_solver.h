@@ -1,7 +1,7 @@
 /*
- * caffe_solver.h -- C ABI of the softmax loss layer and of the stochastic
- * gradient descent update, in the same library as caffe_conv.h
- * (libcaffe_conv.so).
+ * caffe_solver.h -- C ABI of the softmax loss layer, of the stochastic
+ * gradient descent update and of the orthogonalised ("Muon") update, in the
+ * same library as caffe_conv.h (libcaffe_conv.so).
  *
  * The paper lists softmax loss among Caffe's layer types (Sec. 3.2): the
  * loss layer that ends a network and produces the objective and its
@@ -28,6 +28,22 @@
  * parameter blob of a network takes its own call (per-blob rates, e.g. a
  * bias multiplier, are the caller's lr).
  *
+ * Orthogonalised update of a weight matrix W (rows x cols, one per group of a
+ * layer), with the Newton-Schulz iteration NS below in place of the gradient:
+ *   V <- momentum * V + G
+ *   U = nesterov ? G + momentum * V : V
+ *   W <- W - lr * (scale * NS(U) + weight_decay * W)
+ * NS keeps the singular vectors of a matrix and brings its singular values
+ * near 1 (for coefficients made for that):
+ *   X_0 = U / (||U||_F + eps)                (transposed if rows > cols)
+ *   X <- a X + (b A + c A A) X,  A = X X^T,  `steps` times
+ * NS of a zero matrix is zero; a NaN or an infinity in U makes the whole
+ * NS(U) NaN.  Its arithmetic is that of float operands: half-precision pairs
+ * of 22 bits, float sums (errors of the float output near 1e-6 of its norm).
+ * The pairs hold a fixed range: an element of X_0 has an absolute error of
+ * 2^-39, so parts of U more than 2^20 below ||U||_F + eps lose relative
+ * accuracy.
+ *
  * Learning-rate schedules at iteration t >= 0 (0 for the first update),
  * evaluated on the host in double precision:
  *   CAFFE_LR_FIXED  base_lr
@@ -45,6 +61,8 @@
 
 #include <stddef.h>
 #include <stdint.h>
+
+#include "caffe_conv.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -91,6 +109,41 @@ int caffe_sgd_update(float* w, const float* g, float* v, int64_t count, float lr
  * the caller writes the iteration's rate to `lr` before each replay. */
 int caffe_sgd_update_device_lr(float* w, const float* g, float* v, int64_t count, const float* lr,
                                float momentum, float weight_decay, void* stream);
+
+/* `batch` matrices of rows x cols, dense and row-major one after the other
+ * (the weight blob of a convolution: batch = group, rows = K / group, cols =
+ * (C / group) * kernel_h * kernel_w). */
+typedef struct caffe_ns_desc {
+    int32_t batch;      /* >= 0 */
+    int32_t rows, cols; /* 1 .. 2^20 */
+    int32_t steps;      /* 1 .. 64 */
+    float a, b, c;      /* q(t) = a + b t + c t^2; usual: 3.4445, -4.7750, 2.0315 */
+    float eps;          /* >= 0 */
+    int32_t dtype;      /* caffe_newton_schulz: CAFFE_F32 or CAFFE_BF16, of input and
+                           output; caffe_muon_update: CAFFE_F32 */
+} caffe_ns_desc;
+
+/* Host-only: bytes of device workspace (256-byte aligned) of the calls below.
+ * CAFFE_ERR_UNSUPPORTED for coefficients with which t q(t)^2, t the square of
+ * a singular value, starting in [0, 1], or |q| can pass 1024 within `steps`
+ * (a diverging iteration). */
+int caffe_newton_schulz_workspace_size(const caffe_ns_desc* desc, size_t* bytes);
+
+/* out = NS(in) for each matrix.  out may be in. */
+int caffe_newton_schulz(const caffe_ns_desc* desc, const void* in, void* out, void* workspace,
+                        size_t ws_bytes, void* stream);
+
+/* The update above, in place on w and v (batch * rows * cols floats each; g is
+ * read only).  w, g and v must not overlap. */
+int caffe_muon_update(const caffe_ns_desc* desc, float* w, const float* g, float* v, float lr,
+                      float momentum, float weight_decay, float scale, int32_t nesterov,
+                      void* workspace, size_t ws_bytes, void* stream);
+
+/* The same with the learning rate read from device memory when the kernel
+ * runs (as caffe_sgd_update_device_lr). */
+int caffe_muon_update_device_lr(const caffe_ns_desc* desc, float* w, const float* g, float* v,
+                                const float* lr, float momentum, float weight_decay, float scale,
+                                int32_t nesterov, void* workspace, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

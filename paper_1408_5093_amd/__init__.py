@@ -2,8 +2,9 @@
 
 The layer (paper Sec. 3.2: forward pass, and a backward pass giving the
 parameter and input gradients) runs entirely in the HIP kernels of
-``libcaffe_conv.so`` behind the C ABI in ``include/caffe_conv.h`` and
-``include/caffe_layers.h``.  This module only marshals arguments: it takes
+``libcaffe_conv.so`` behind the C ABI in ``include/caffe_conv.h``,
+``include/caffe_layers.h``, ``include/caffe_solver.h`` and
+``include/caffe_int8.h``.  This module only marshals arguments: it takes
 PyTorch device tensors, checks dtype/device/contiguity, and passes their data
 pointers and the current HIP stream.  The functions named ``caffe_*`` take
 the same arguments as their C counterparts; the short names allocate outputs
@@ -23,7 +24,7 @@ from ._lib import (  # noqa: F401
     CAFFE_LR_FIXED, CAFFE_LR_INV, CAFFE_LR_STEP, LrSchedule, PASS_BACKWARD,
     PASS_BACKWARD_DATA, PASS_BACKWARD_POOL_LRN, PASS_BACKWARD_WEIGHTS, PASS_FORWARD,
     POOL_LRN_STAGE_ONLY, POOL_MASK_OFFSETS, POOL_RELU_INPUT, CaffeError, ConvDesc,
-    LrnDesc, PoolDesc, check, load, LIB_PATH,
+    LrnDesc, PoolDesc, check, load, LIB_PATH, CAFFE_INT8_ROWS, Ip8Desc, NsDesc,
 )
 
 __all__ = [
@@ -33,6 +34,7 @@ __all__ = [
     "sgd_learning_rate", "softmax_loss", "sgd_update", "pool_lrn_forward", "lrn_pool_backward",
     "pool_lrn_supported", "caffe_conv_backward_pool_lrn", "relu_backward",
     "caffe_conv_backward_into", "conv_stage_below_supported", "pool_lrn_stage_supported",
+    "newton_schulz", "muon_update", "quantize_rows", "inner_product_int8", "int8_pitch",
 ]
 
 
@@ -503,3 +505,178 @@ def sgd_update(w, g, v, lr, momentum=0.0, weight_decay=0.0, stream=None):
         return
     check(load().caffe_sgd_update(_ptr(w), _ptr(g), _ptr(v), w.numel(), float(lr),
                                   float(momentum), float(weight_decay), _stream(stream)))
+
+
+# ------------------------------------------------- orthogonalised updates
+NS_COEF = (3.4445, -4.7750, 2.0315)  # a, b, c of the quintic step a x + b x^3 + c x^5
+
+
+def ns_desc(shape, steps=5, coef=NS_COEF, eps=1e-7, group=1, dtype=CAFFE_F32):
+    """Descriptor for a weight blob: (rows, cols), (batch, rows, cols), or (K,
+    C/group, kh, kw), whose groups are matrices of K/group x (C/group kh kw)."""
+    shape = tuple(int(v) for v in shape)
+    if len(shape) == 3:
+        if group != 1:
+            raise ValueError("group goes with a 2-D or 4-D weight")
+        batch, rows, cols = shape
+    elif len(shape) in (2, 4):
+        if group < 1 or shape[0] % group:
+            raise ValueError(f"group {group} must divide {shape[0]} rows")
+        batch, rows, cols = group, shape[0] // group, 1
+        for v in shape[1:]:
+            cols *= v
+    else:
+        raise ValueError(f"a matrix, a batch of matrices or a 4-D weight blob, not {shape}")
+    return NsDesc(batch, rows, cols, int(steps), *(float(v) for v in coef), float(eps),
+                  int(dtype))
+
+
+def newton_schulz_workspace_size(desc):
+    n = ctypes.c_size_t()
+    check(load().caffe_newton_schulz_workspace_size(ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def _same_device(first, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("tensors are on different devices")
+
+
+def newton_schulz(g, steps=5, coef=NS_COEF, eps=1e-7, group=1, out=None, ws=None, stream=None):
+    """Each matrix of g (see ns_desc; float32 or bfloat16) brought near its
+    nearest semi-orthogonal matrix by `steps` Newton-Schulz products."""
+    if g.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"in must be float32 or bfloat16, got {g.dtype}")
+    _dev(g, "in", g.dtype)
+    d = ns_desc(g.shape, steps, coef, eps, group,
+                CAFFE_BF16 if g.dtype == torch.bfloat16 else CAFFE_F32)
+    if out is None:
+        out = torch.empty_like(g)
+    _dev(out, "out", g.dtype)
+    if out.shape != g.shape:
+        raise ValueError("in and out differ in shape")
+    _same_device(g, out)
+    with torch.cuda.device(g.device):
+        buf = (ws or Workspace(g.device)).get(newton_schulz_workspace_size(d))
+        check(load().caffe_newton_schulz(ctypes.byref(d), _ptr(g), _ptr(out), _ptr(buf),
+                                         0 if buf is None else buf.numel(), _stream(stream)))
+    return out
+
+
+def muon_update(w, g, v, lr, momentum=0.95, weight_decay=0.0, nesterov=True, scale=None, steps=5,
+                coef=NS_COEF, eps=1e-7, group=1, ws=None, stream=None):
+    """In place: v <- momentum v + g; u = nesterov ? g + momentum v : v;
+    w <- w - lr (scale newton_schulz(u) + weight_decay w).  `scale` defaults to
+    sqrt(max(1, rows / cols)).  `lr` is a number, or a one-element float32
+    device tensor read when the kernel runs (for graph capture)."""
+    for t, n in ((w, "w"), (g, "g"), (v, "v")):
+        _dev(t, n, torch.float32)
+    if not (w.shape == g.shape == v.shape):
+        raise ValueError("w, g and v must have the same shape")
+    d = ns_desc(w.shape, steps, coef, eps, group)
+    if scale is None:
+        scale = max(1.0, d.rows / max(1, d.cols)) ** 0.5
+    lib = load()
+    _same_device(w, g, v, lr if isinstance(lr, torch.Tensor) else None)
+    with torch.cuda.device(w.device):
+        buf = (ws or Workspace(w.device)).get(newton_schulz_workspace_size(d))
+        tail = (float(momentum), float(weight_decay), float(scale), int(bool(nesterov)),
+                _ptr(buf), 0 if buf is None else buf.numel(), _stream(stream))
+        if isinstance(lr, torch.Tensor):
+            _dev(lr, "lr", torch.float32)
+            if lr.numel() != 1:
+                raise ValueError("lr must have one element")
+            check(lib.caffe_muon_update_device_lr(ctypes.byref(d), _ptr(w), _ptr(g), _ptr(v),
+                                                  _ptr(lr), *tail))
+        else:
+            check(lib.caffe_muon_update(ctypes.byref(d), _ptr(w), _ptr(g), _ptr(v), float(lr),
+                                        *tail))
+
+
+# ------------------------------------------------------------- 8-bit rows
+def int8_pitch(cols):
+    """Bytes between 8-bit rows of `cols` values."""
+    p = load().caffe_int8_pitch(int(cols))
+    if p == 0:
+        raise ValueError(f"8-bit rows hold 1 to 2^17 values, not {cols}")
+    return p
+
+
+_ROW_TYPES = {torch.float32: CAFFE_F32, torch.bfloat16: CAFFE_BF16}
+
+
+def quantize_rows(x, q=None, scale=None, stream=None):
+    """x (rows, ...) float32 or bfloat16, e.g. an inner product's weight or its
+    bottom -> (q, scale): int8 rows padded with zeros to int8_pitch(cols)
+    bytes, and float32 scales, with x[r] near q[r, :cols] * scale[r]."""
+    if x.dtype not in _ROW_TYPES:
+        raise ValueError(f"x must be float32 or bfloat16, got {x.dtype}")
+    _dev(x, "x", x.dtype)
+    if x.dim() < 2:
+        raise ValueError("x must have rows and columns")
+    rows, cols = x.shape[0], x[0].numel() if x.shape[0] else int(torch.tensor(x.shape[1:]).prod())
+    pitch = int8_pitch(cols)
+    if q is None:
+        q = torch.empty((rows, pitch), dtype=torch.int8, device=x.device)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _dev(q, "q", torch.int8), _dev(scale, "scale", torch.float32)
+    if tuple(q.shape) != (rows, pitch) or scale.numel() != rows:
+        raise ValueError(f"q must be {(rows, pitch)} and scale {(rows,)}")
+    _same_device(x, q, scale)
+    with torch.cuda.device(x.device):
+        check(load().caffe_quantize_rows(_ptr(x), _ROW_TYPES[x.dtype], rows, cols, _ptr(q),
+                                         _ptr(scale), _stream(stream)))
+    return q, scale
+
+
+def inner_product_int8(x, weight, weight_scale, bias=None, C=None, x_scale=None, relu=False,
+                       top_dtype=torch.float32, out=None, ws=None, stream=None):
+    """top (N, K) = x weight^T + bias, in 8 bits: weight and weight_scale as
+    quantize_rows makes them; x (N, ...) of C values a sample in float32 or
+    bfloat16 (brought to 8-bit rows in the call), or int8 rows with x_scale.
+    C (the values of a row) may be left out for a float x."""
+    rows8 = x.dtype == torch.int8
+    if not rows8 and x.dtype not in _ROW_TYPES:
+        raise ValueError(f"bottom must be float32, bfloat16 or int8, got {x.dtype}")
+    _dev(x, "bottom", x.dtype), _dev(weight, "weight", torch.int8)
+    _dev(weight_scale, "weight_scale", torch.float32), _dev(bias, "bias", torch.float32)
+    _dev(x_scale, "bottom_scale", torch.float32)
+    if top_dtype not in _ROW_TYPES:
+        raise ValueError(f"top must be float32 or bfloat16, got {top_dtype}")
+    N = x.shape[0]
+    if x.dim() < 2 or weight.dim() != 2:
+        raise ValueError("bottom must have rows, weight (K, pitch)")
+    per = 1
+    for v in x.shape[1:]:
+        per *= int(v)
+    if C is None:
+        if rows8:
+            raise ValueError("8-bit rows need C, the values of a row")
+        C = per
+    pitch, K = int8_pitch(C), weight.shape[0]
+    if weight.shape[1] != pitch or per != (pitch if rows8 else C):
+        raise ValueError(f"rows of C={C} values take {pitch} bytes: weight {tuple(weight.shape)}, "
+                         f"bottom {tuple(x.shape)}")
+    if rows8 != (x_scale is not None) or (rows8 and x_scale.numel() != N):
+        raise ValueError("x_scale goes with int8 rows, one for each")
+    if weight_scale.numel() != K or (bias is not None and bias.numel() != K):
+        raise ValueError(f"weight_scale and bias must have K={K} elements")
+    if out is None:
+        out = torch.empty((N, K), dtype=top_dtype, device=x.device)
+    _dev(out, "top", top_dtype)
+    if out.numel() != N * K:
+        raise ValueError(f"top must have {N} x {K} elements")
+    _same_device(x, weight, weight_scale, bias, x_scale, out)
+    d = Ip8Desc(N, int(C), K, int(bool(relu)), CAFFE_INT8_ROWS if rows8 else _ROW_TYPES[x.dtype],
+                _ROW_TYPES[top_dtype])
+    lib = load()
+    with torch.cuda.device(x.device):
+        n = ctypes.c_size_t()
+        check(lib.caffe_inner_product_int8_workspace_size(ctypes.byref(d), ctypes.byref(n)))
+        buf = (ws or Workspace(x.device)).get(n.value)
+        check(lib.caffe_inner_product_int8(
+            ctypes.byref(d), _ptr(x), _ptr(x_scale), _ptr(weight), _ptr(weight_scale), _ptr(bias),
+            _ptr(out), _ptr(buf), 0 if buf is None else buf.numel(), _stream(stream)))
+    return out

@@ -20,6 +20,7 @@ CAFFE_ERR_HIP = -5
 CAFFE_F32 = 0
 CAFFE_BF16 = 1
 CAFFE_BF16_F32_BOTTOM = 2
+CAFFE_INT8_ROWS = 16
 
 BACKWARD_TOP_DIFF_MASKED = 1
 BACKWARD_MASK_BOTTOM_DIFF = 2
@@ -60,6 +61,9 @@ EXPORTS = (
     "caffe_conv_backward_pool_lrn_ex", "caffe_conv_backward_into",
     "caffe_conv_stage_below_supported", "caffe_conv_forward_ex", "caffe_pool_lrn_forward_into",
     "caffe_pool_lrn_stage_supported", "caffe_lrn_pool_backward_ex",
+    "caffe_newton_schulz_workspace_size", "caffe_newton_schulz", "caffe_muon_update",
+    "caffe_muon_update_device_lr", "caffe_int8_pitch", "caffe_quantize_rows",
+    "caffe_inner_product_int8_workspace_size", "caffe_inner_product_int8",
 )
 
 
@@ -86,6 +90,16 @@ class LrSchedule(ctypes.Structure):
                 ("stepsize", ctypes.c_int32)]
 
 
+class NsDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float),
+                ("c", ctypes.c_float), ("eps", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+class Ip8Desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("N", "C", "K", "relu", "bottom_type", "top_type")]
+
+
 class CaffeError(RuntimeError):
     def __init__(self, status, message):
         super().__init__(f"{message} ({status})")
@@ -110,6 +124,8 @@ def load():
     lib = ctypes.CDLL(LIB_PATH)
     vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     cdp, pdp, ldp = ctypes.POINTER(ConvDesc), ctypes.POINTER(PoolDesc), ctypes.POINTER(LrnDesc)
+    ndp, idp = ctypes.POINTER(NsDesc), ctypes.POINTER(Ip8Desc)
+    f32 = ctypes.c_float
     pi32 = ctypes.POINTER(i32)
     sig = {
         "caffe_conv_out_shape": [cdp, pi32, pi32],
@@ -148,6 +164,14 @@ def load():
         "caffe_sgd_update": [vp, vp, vp, i64, ctypes.c_float, ctypes.c_float, ctypes.c_float,
                              vp],
         "caffe_sgd_update_device_lr": [vp, vp, vp, i64, vp, ctypes.c_float, ctypes.c_float, vp],
+        "caffe_newton_schulz_workspace_size": [ndp, ctypes.POINTER(sz)],
+        "caffe_newton_schulz": [ndp, vp, vp, vp, sz, vp],
+        "caffe_muon_update": [ndp, vp, vp, vp, f32, f32, f32, f32, i32, vp, sz, vp],
+        "caffe_muon_update_device_lr": [ndp, vp, vp, vp, vp, f32, f32, f32, i32, vp, sz, vp],
+        "caffe_int8_pitch": [i32],
+        "caffe_quantize_rows": [vp, i32, i64, i32, vp, vp, vp],
+        "caffe_inner_product_int8_workspace_size": [idp, ctypes.POINTER(sz)],
+        "caffe_inner_product_int8": [idp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
     }
     for name, args in sig.items():
         f = getattr(lib, name)

@@ -38,6 +38,8 @@ EXTRA = {
     "conv_wgrad.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "conv_triple.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "conv_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "muon.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "int8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 

@@ -14,6 +14,7 @@
 #include <mutex>
 
 #include "../../include/caffe_conv.h"
+#include "../../include/caffe_int8.h"
 #include "../../include/caffe_layers.h"
 #include "../../include/caffe_solver.h"
 #include "kernels.h"
@@ -2783,6 +2784,218 @@ int caffe_sgd_update_device_lr(float* w, const float* g, float* v, int64_t count
         return fail(CAFFE_ERR_ALIGN, "lr is not 4-byte aligned");
     LAUNCH(launch_sgd_update(w, g, v, count, 0.f, lr, momentum, weight_decay, (hipStream_t)stream),
            "SGD update launch");
+    return CAFFE_OK;
+}
+
+// ----------------------------------------------------- orthogonalised updates
+static int plan_ns(const caffe_ns_desc* d, NsPlan* q)
+{
+    if (!d)
+        return fail(CAFFE_ERR_INVALID_ARG, "desc is NULL");
+    if (d->batch < 0 || d->rows < 1 || d->cols < 1)
+        return fail(CAFFE_ERR_INVALID_ARG, "batch must be >= 0, rows and cols >= 1: %d x %d x %d",
+                    d->batch, d->rows, d->cols);
+    if (d->steps < 1)
+        return fail(CAFFE_ERR_INVALID_ARG, "steps must be >= 1");
+    if (!std::isfinite(d->a) || !std::isfinite(d->b) || !std::isfinite(d->c) ||
+        !std::isfinite(d->eps) || d->eps < 0.f)
+        return fail(CAFFE_ERR_INVALID_ARG, "coefficients must be finite, eps >= 0");
+    if (d->rows > (1 << 20) || d->cols > (1 << 20) || d->batch > 65535)
+        return fail(CAFFE_ERR_UNSUPPORTED, "rows and cols must be <= 2^20, batch <= 65535");
+    if (d->steps > kNsMaxSteps)
+        return fail(CAFFE_ERR_UNSUPPORTED, "steps must be <= %d", kNsMaxSteps);
+    if (d->dtype != CAFFE_F32 && d->dtype != CAFFE_BF16)
+        return fail(CAFFE_ERR_UNSUPPORTED, "unknown dtype %d", d->dtype);
+    if (!ns_plan(d->batch, d->rows, d->cols, d->steps, d->a, d->b, d->c, q))
+        return fail(CAFFE_ERR_UNSUPPORTED, "the iteration can leave its range: a=%g b=%g c=%g "
+                    "over %d steps", d->a, d->b, d->c, d->steps);
+    return CAFFE_OK;
+}
+
+static NsArgs ns_args(const caffe_ns_desc* d)
+{
+    NsArgs x{};
+    x.a = d->a;
+    x.b = d->b;
+    x.c = d->c;
+    x.eps = d->eps;
+    x.bf16 = d->dtype == CAFFE_BF16;
+    return x;
+}
+
+int caffe_newton_schulz_workspace_size(const caffe_ns_desc* desc, size_t* bytes)
+{
+    NsPlan q;
+    CHECK(plan_ns(desc, &q));
+    if (!bytes)
+        return fail(CAFFE_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = q.ws_bytes;
+    return CAFFE_OK;
+}
+
+int caffe_newton_schulz(const caffe_ns_desc* desc, const void* in, void* out, void* workspace,
+                        size_t ws_bytes, void* stream)
+{
+    NsPlan q;
+    CHECK(plan_ns(desc, &q));
+    CHECK(check_ptr(in, q.batch > 0, "in"));
+    CHECK(check_ptr(out, q.batch > 0, "out"));
+    CHECK(check_ws(workspace, ws_bytes, q.ws_bytes));
+    NsArgs x = ns_args(desc);
+    x.g = in;
+    x.out = out;
+    LAUNCH(launch_newton_schulz(q, x, (char*)workspace, (hipStream_t)stream),
+           "Newton-Schulz launch");
+    return CAFFE_OK;
+}
+
+static int muon_update(const caffe_ns_desc* desc, float* w, const float* g, float* v, float lr,
+                       const float* lr_dev, float momentum, float weight_decay, float scale,
+                       int32_t nesterov, void* workspace, size_t ws_bytes, void* stream)
+{
+    NsPlan q;
+    CHECK(plan_ns(desc, &q));
+    if (desc->dtype != CAFFE_F32)
+        return fail(CAFFE_ERR_UNSUPPORTED, "the update takes CAFFE_F32");
+    if (!std::isfinite(lr) || !std::isfinite(momentum) || !std::isfinite(weight_decay) ||
+        !std::isfinite(scale))
+        return fail(CAFFE_ERR_INVALID_ARG, "lr, momentum, weight_decay and scale must be finite");
+    if (nesterov != 0 && nesterov != 1)
+        return fail(CAFFE_ERR_INVALID_ARG, "nesterov must be 0 or 1");
+    const bool nz = q.batch > 0;
+    CHECK(check_ptr(w, nz, "w"));
+    CHECK(check_ptr(g, nz, "g"));
+    CHECK(check_ptr(v, nz, "v"));
+    CHECK(check_ws(workspace, ws_bytes, q.ws_bytes));
+    NsArgs x = ns_args(desc);
+    x.g = g;
+    x.v = v;
+    x.w = w;
+    x.lr = lr;
+    x.lr_dev = lr_dev;
+    x.momentum = momentum;
+    x.decay = weight_decay;
+    x.step_scale = scale;
+    x.nesterov = nesterov;
+    LAUNCH(launch_newton_schulz(q, x, (char*)workspace, (hipStream_t)stream),
+           "orthogonalised update launch");
+    return CAFFE_OK;
+}
+
+int caffe_muon_update(const caffe_ns_desc* desc, float* w, const float* g, float* v, float lr,
+                      float momentum, float weight_decay, float scale, int32_t nesterov,
+                      void* workspace, size_t ws_bytes, void* stream)
+{
+    return muon_update(desc, w, g, v, lr, nullptr, momentum, weight_decay, scale, nesterov,
+                       workspace, ws_bytes, stream);
+}
+
+int caffe_muon_update_device_lr(const caffe_ns_desc* desc, float* w, const float* g, float* v,
+                                const float* lr, float momentum, float weight_decay, float scale,
+                                int32_t nesterov, void* workspace, size_t ws_bytes, void* stream)
+{
+    if (!lr)
+        return fail(CAFFE_ERR_INVALID_ARG, "lr is NULL");
+    if (!aligned(lr, 4))
+        return fail(CAFFE_ERR_ALIGN, "lr is not 4-byte aligned");
+    return muon_update(desc, w, g, v, 0.f, lr, momentum, weight_decay, scale, nesterov, workspace,
+                       ws_bytes, stream);
+}
+
+// ------------------------------------------------------------------ 8-bit rows
+int32_t caffe_int8_pitch(int32_t cols)
+{
+    return cols < 1 || cols > (1 << 17) ? 0 : (cols + 127) / 128 * 128;
+}
+
+int caffe_quantize_rows(const void* x, int32_t dtype, int64_t rows, int32_t cols, int8_t* q,
+                        float* scale, void* stream)
+{
+    if (rows < 0 || cols < 1)
+        return fail(CAFFE_ERR_INVALID_ARG, "rows must be >= 0 and cols >= 1");
+    if (rows > INT32_MAX || caffe_int8_pitch(cols) == 0)
+        return fail(CAFFE_ERR_UNSUPPORTED, "rows must be < 2^31 and cols <= 2^17");
+    if (dtype != CAFFE_F32 && dtype != CAFFE_BF16)
+        return fail(CAFFE_ERR_UNSUPPORTED, "unknown dtype %d", dtype);
+    CHECK(check_ptr(x, rows > 0, "x"));
+    CHECK(check_ptr(q, rows > 0, "q"));
+    CHECK(check_ptr(scale, rows > 0, "scale"));
+    LAUNCH(launch_quantize_rows(x, dtype == CAFFE_BF16, rows, cols, caffe_int8_pitch(cols), q,
+                                scale, (hipStream_t)stream),
+           "row quantisation launch");
+    return CAFFE_OK;
+}
+
+static int check_ip8(const caffe_ip8_desc* d)
+{
+    if (!d)
+        return fail(CAFFE_ERR_INVALID_ARG, "desc is NULL");
+    if (d->N < 0 || d->C < 1 || d->K < 1)
+        return fail(CAFFE_ERR_INVALID_ARG, "N must be >= 0, C and K >= 1: N=%d C=%d K=%d", d->N,
+                    d->C, d->K);
+    if (d->relu != 0 && d->relu != 1)
+        return fail(CAFFE_ERR_INVALID_ARG, "relu must be 0 or 1");
+    if (d->bottom_type != CAFFE_F32 && d->bottom_type != CAFFE_BF16 &&
+        d->bottom_type != CAFFE_INT8_ROWS)
+        return fail(CAFFE_ERR_UNSUPPORTED, "unknown bottom type %d", d->bottom_type);
+    if (d->top_type != CAFFE_F32 && d->top_type != CAFFE_BF16)
+        return fail(CAFFE_ERR_UNSUPPORTED, "unknown top type %d", d->top_type);
+    if (caffe_int8_pitch(d->C) == 0)
+        return fail(CAFFE_ERR_UNSUPPORTED, "C must be <= 2^17 (exact 32-bit sums)");
+    if (d->N > (1 << 30) || d->K > (1 << 30) || ((int64_t)d->N / 64 + 1) * (d->K / 64 + 1) > (1 << 30))
+        return fail(CAFFE_ERR_UNSUPPORTED, "N x K has more than 2^30 tiles of 64 x 64");
+    return CAFFE_OK;
+}
+
+static size_t ip8_ws(const caffe_ip8_desc* d)
+{
+    return d->bottom_type == CAFFE_INT8_ROWS
+               ? 0
+               : (size_t)d->N * caffe_int8_pitch(d->C) + (size_t)d->N * sizeof(float);
+}
+
+int caffe_inner_product_int8_workspace_size(const caffe_ip8_desc* desc, size_t* bytes)
+{
+    CHECK(check_ip8(desc));
+    if (!bytes)
+        return fail(CAFFE_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = ip8_ws(desc);
+    return CAFFE_OK;
+}
+
+int caffe_inner_product_int8(const caffe_ip8_desc* desc, const void* bottom,
+                             const float* bottom_scale, const int8_t* weight,
+                             const float* weight_scale, const float* bias, void* top,
+                             void* workspace, size_t ws_bytes, void* stream)
+{
+    CHECK(check_ip8(desc));
+    const bool nz = desc->N > 0, rows8 = desc->bottom_type == CAFFE_INT8_ROWS;
+    CHECK(check_ptr(bottom, nz, "bottom"));
+    CHECK(check_ptr(bottom_scale, nz && rows8, "bottom_scale"));
+    if (bottom_scale && !rows8)
+        return fail(CAFFE_ERR_INVALID_ARG, "bottom_scale given for a bottom that is not in 8 bits");
+    CHECK(check_ptr(weight, nz, "weight"));
+    CHECK(check_ptr(weight_scale, nz, "weight_scale"));
+    CHECK(check_ptr(bias, false, "bias"));
+    CHECK(check_ptr(top, nz, "top"));
+    CHECK(check_ws(workspace, ws_bytes, ip8_ws(desc)));
+    Ip8Args a{};
+    a.N = desc->N;
+    a.C = desc->C;
+    a.K = desc->K;
+    a.pitch = caffe_int8_pitch(desc->C);
+    a.relu = desc->relu;
+    a.bottom_type = rows8 ? kIp8BottomInt8
+                          : (desc->bottom_type == CAFFE_BF16 ? kIp8BottomBf16 : kIp8BottomF32);
+    a.top_bf16 = desc->top_type == CAFFE_BF16;
+    a.bottom = bottom;
+    a.bottom_scale = bottom_scale;
+    a.weight = weight;
+    a.weight_scale = weight_scale;
+    a.bias = bias;
+    a.top = top;
+    LAUNCH(launch_inner_product_int8(a, (char*)workspace, (hipStream_t)stream),
+           "8-bit inner product launch");
     return CAFFE_OK;
 }
 

@@ -545,4 +545,49 @@ hipError_t launch_softmax_loss(const float* z, const int32_t* labels, int N, int
 hipError_t launch_sgd_update(float* w, const float* g, float* v, int64_t count, float lr,
                              const float* lr_dev, float momentum, float decay, hipStream_t s);
 
+// ---- orthogonalised updates (muon.hip)
+constexpr int kNsMaxSteps = 64;
+constexpr double kNsMaxRange = 1024.0;  // of the iteration's singular values squared, and of q
+// Newton-Schulz iteration on `batch` matrices of rows x cols: m x n with
+// m <= n after a transpose (tall), its segments, the bounds that fix the
+// operands' scales, and the workspace.
+struct NsPlan {
+    int batch, rows, cols, m, n, tall, steps, segments, splits, norm_blocks;
+    double bound[kNsMaxSteps + 1];  // of the squared singular values before step k
+    double qmax[kNsMaxSteps];       // of |q| over them
+    int length[kNsMaxSteps];        // steps of each segment
+    size_t m_pitch, n_pitch;        // bytes of a row of m (n) elements in two terms
+    size_t mm_bytes, xr_bytes, xt_bytes;
+    size_t off_part, off_split, off_xr, off_xt[2], off_mm[5], ws_bytes;
+};
+// false: the coefficients let the iteration leave kNsMaxRange.
+bool ns_plan(int batch, int rows, int cols, int steps, float a, float b, float c, NsPlan* plan);
+struct NsArgs {
+    const void* g;  // float, or bfloat16 with bf16
+    int bf16;
+    float a, b, c, eps;
+    void* out;      // the orthogonalised matrix (g's type), or with w the step on w:
+    float *w, *v;   // v <- momentum v + g; w <- w - lr (step_scale O + decay w)
+    const float* lr_dev;
+    float lr, momentum, decay, step_scale;
+    int nesterov;
+};
+hipError_t launch_newton_schulz(const NsPlan& plan, const NsArgs& args, char* ws, hipStream_t s);
+
+// ---- 8-bit rows (int8.hip)
+// q: rows of `pitch` bytes (cols, padded with zeros), scale: one per row.
+hipError_t launch_quantize_rows(const void* x, int bf16, int64_t rows, int cols, int pitch,
+                                int8_t* q, float* scale, hipStream_t s);
+enum { kIp8BottomF32 = 0, kIp8BottomBf16 = 1, kIp8BottomInt8 = 2 };
+struct Ip8Args {
+    int N, C, K, pitch, relu, bottom_type, top_bf16;
+    const void* bottom;          // N x C, or N rows of pitch bytes with bottom_scale
+    const float* bottom_scale;
+    const int8_t* weight;        // K rows of pitch bytes
+    const float *weight_scale, *bias;
+    void* top;                   // N x K
+};
+// ws: N * pitch + 4 N bytes for a bottom that is not in 8 bits.
+hipError_t launch_inner_product_int8(const Ip8Args& args, char* ws, hipStream_t s);
+
 }  // namespace caffe_hip

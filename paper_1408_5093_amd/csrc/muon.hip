@@ -1,0 +1,759 @@
+// muon.hip -- the Newton-Schulz orthogonalisation of weight matrices and the
+// parameter update that steps along its result.
+//
+// Mathematics.  For G (m x n, m <= n; a taller matrix is taken transposed)
+//   X_0 = G / (||G||_F + eps),   X <- (a I + b A + c A^2) X,  A = X X^T
+// keeps the singular vectors of G and maps each singular value s by
+// s q(s^2), q(t) = a + b t + c t^2.  Every factor on the left is a polynomial
+// of the same m x m matrix, so a segment of L steps needs the wide matrix
+// only at its ends: with R = X X^T,
+//   Q = a I + b R + c R R,  T = Q R,  R <- T Q,  P <- Q P     (L times)
+// and then X <- P X.  All of these are symmetric and commute, so one half of
+// each is computed and mirrored.  Per segment 3 m^2 n + (4 L - 3) m^3
+// operations against L (3 m^2 n + m^3) for the steps one by one.
+//
+// Segments are short because the Gram matrix holds the squares of the
+// singular values: a rounding error of R grows by q(0)^2 per step in the
+// directions whose values are still small.  The first segment, where the
+// trace of R is 1, ends before max|q|^(2 (L - 1)) passes 2^8 (three steps of
+// the usual quintic), a later one, where R has the singular values near 1 of
+// many directions, before it passes 2^4 (two).  Errors of the iteration in
+// float arithmetic, 1000 x 1024, relative 2-norm: five steps 1.6e-6 step by
+// step, 2.5e-5 in one segment, 4.6e-6 as 3 + 2; six steps 2.3e-6, 1.1e-4,
+// 2.0e-5 as 3 + 3 and 3.7e-6 as 2 + 2 + 2.
+//
+// Precision.  The products run on the half-precision matrix instructions with
+// float accumulators, each operand as the sum of two half terms (22 bits; the
+// low term is a multiple of 2^-24 at the least, so the sum has an absolute
+// error of 2^-25 on the operand's scale).  The scales are powers of two from
+// bounds on the iterates: t in [0, 1] at the start, t q(t)^2 after a step, so
+// no element can leave the half type's range, whatever the matrix.  Three
+// products (high high, high low, low high) give the accuracy of a float
+// product: the missing low low term is 2^-22 of it.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "tile_gemm.h"
+
+namespace caffe_hip {
+
+namespace {
+
+typedef _Float16 halfx4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+
+// ------------------------------------------------------------ pair matrices
+// Element (row, k): line k / 32 of the row, its high half at byte 2 (k % 32),
+// its low half 64 bytes on.  k a multiple of 4.
+__device__ __forceinline__ size_t pair_off(size_t pitch, int row, int k)
+{
+    return (size_t)row * pitch + (size_t)(k >> 5) * 128 + (k & 31) * 2;
+}
+
+__device__ __forceinline__ void store_pair4(char* M, size_t off, const float (&v)[4])
+{
+    halfx4 h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        h[e] = (_Float16)v[e];
+        l[e] = (_Float16)(v[e] - (float)h[e]);
+    }
+    *(halfx4*)(M + off) = h;
+    *(halfx4*)(M + off + 64) = l;
+}
+
+__device__ __forceinline__ void load_pair4(const char* M, size_t off, float (&v)[4])
+{
+    const halfx4 h = *(const halfx4*)(M + off), l = *(const halfx4*)(M + off + 64);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        v[e] = (float)h[e] + (float)l[e];
+}
+
+// --------------------------------------------------------------- first pass
+// u (the matrix to orthogonalise) is g, or with momentum
+// v <- mu v + g (written) and u = nesterov ? g + mu v : v.
+struct NsInput {
+    const void* g;
+    float* v;       // null: u = g
+    float mu;
+    int nesterov;
+    int bf16;       // g is bfloat16 (v null)
+    int64_t count;  // elements of one matrix
+};
+
+template <int VEC>
+__device__ __forceinline__ void load_vec(const NsInput& in, int64_t at, float (&g)[VEC])
+{
+    if (in.bf16) {
+        const uint16_t* p = (const uint16_t*)in.g + at;
+        if constexpr (VEC == 4) {
+            const u16x4 x = *(const u16x4*)p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                g[e] = bf16_to_f32(x[e]);
+        } else {
+            g[0] = bf16_to_f32(*p);
+        }
+    } else {
+        const float* p = (const float*)in.g + at;
+        if constexpr (VEC == 4) {
+            const floatx4 x = *(const floatx4*)p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                g[e] = x[e];
+        } else {
+            g[0] = *p;
+        }
+    }
+}
+
+template <int VEC>
+__device__ __forceinline__ void load_u(const NsInput& in, int64_t at, bool update, float (&u)[VEC])
+{
+    load_vec<VEC>(in, at, u);
+    if (in.v) {
+        float* p = in.v + at;
+        float v[VEC];
+        if constexpr (VEC == 4) {
+            const floatx4 x = *(const floatx4*)p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = x[e];
+        } else {
+            v[0] = *p;
+        }
+        if (update) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                v[e] = in.mu * v[e] + u[e];
+            if constexpr (VEC == 4)
+                *(floatx4*)p = floatx4{v[0], v[1], v[2], v[3]};
+            else
+                *p = v[0];
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            u[e] = in.nesterov ? u[e] + in.mu * v[e] : v[e];
+    }
+}
+
+constexpr int kNormBlocks = 256;  // partial sums of one matrix, at most
+
+__device__ __forceinline__ double block_sum(double s)
+{
+    __shared__ double part[4];
+    for (int off = 32; off > 0; off >>= 1)
+        s += __shfl_xor(s, off, 64);
+    if ((threadIdx.x & 63) == 0)
+        part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = (part[0] + part[1]) + (part[2] + part[3]);
+    return s;
+}
+
+// The momentum update and each block's part of ||u||^2, in double (squares of
+// floats neither overflow nor vanish there).  Bound by HBM.
+template <int VEC>
+__global__ void __launch_bounds__(256)
+ns_norm_kernel(const NsInput in, double* __restrict__ part)
+{
+    const int64_t base = (int64_t)blockIdx.y * in.count;
+    double s = 0.0;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC; i < in.count;
+         i += (int64_t)gridDim.x * 256 * VEC) {
+        float u[VEC];
+        load_u<VEC>(in, base + i, true, u);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            s += (double)u[e] * (double)u[e];
+    }
+    s = block_sum(s);
+    if (threadIdx.x == 0)
+        part[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
+}
+
+// 1 / (||u|| + eps), 0 for a zero matrix, NaN where an element is NaN or
+// infinite; the parts are added in a fixed order.
+__device__ __forceinline__ double inv_norm(const double* part, int parts, double eps)
+{
+    const double s = block_sum((int)threadIdx.x < parts ? part[threadIdx.x] : 0.0);
+    return s == 0.0 ? 0.0 : (s < INFINITY ? 1.0 / (sqrt(s) + eps) : NAN);
+}
+
+// u / norm as pair matrices in both orders: rows along u's columns (Nl) and
+// columns along u's rows (Tl), through a 64 x 64 tile in LDS.
+struct NsStage {
+    NsInput in;
+    const double* part;
+    int parts;
+    double eps;
+    int rows, cols;
+    char *Nl, *Tl;
+    size_t n_pitch, t_pitch, n_batch, t_batch;  // bytes
+    float scale;
+};
+
+template <int VEC>
+__global__ void __launch_bounds__(256)
+ns_stage_kernel(const NsStage p)
+{
+    __shared__ float tile[64][65];
+    const int b = blockIdx.z;
+    const double inv = inv_norm(p.part + (size_t)b * p.parts, p.parts, p.eps) * p.scale;
+    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+    const int64_t base = (int64_t)b * p.in.count;
+    const int nk = (int)(p.n_pitch / 4), tk = (int)(p.t_pitch / 4);  // padded reduction lengths
+    const int c4 = (threadIdx.x & 15) * 4, rt = threadIdx.x >> 4;
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int r = r0 + rt + 16 * it, c = c0 + c4;
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+        if (r < p.rows) {
+            const int64_t at = base + (int64_t)r * p.cols + c;
+            if constexpr (VEC == 4) {
+                if (c < p.cols)
+                    load_u<4>(p.in, at, false, x);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < p.cols) {
+                        float y[1];
+                        load_u<1>(p.in, at + e, false, y);
+                        x[e] = y[0];
+                    }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x[e] = (float)((double)x[e] * inv);
+            if (c < nk)
+                store_pair4(p.Nl + b * p.n_batch, pair_off(p.n_pitch, r, c), x);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            tile[rt + 16 * it][c4 + e] = x[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int c = c0 + rt + 16 * it, r = r0 + c4;
+        if (c < p.cols && r < tk) {
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x[e] = tile[c4 + e][rt + 16 * it];
+            store_pair4(p.Tl + b * p.t_batch, pair_off(p.t_pitch, c, r), x);
+        }
+    }
+}
+
+// ----------------------------------------------------------------- products
+enum NsEpi {
+    kEpiSym = 0,   // D = A B, symmetric, mirrored
+    kEpiQ = 1,     // D = a I + b R + c A B, symmetric, mirrored
+    kEpiPart = 2,  // part[split] = A B over a share of the reduction
+    kEpiX = 3,     // D = A B and its transpose D2
+    kEpiOut = 4    // the result, or the weights' step
+};
+
+struct NsGemm {
+    const char *A[2], *B[2];  // two products of the same shape in one launch
+    char* D[2];
+    char* D2;
+    const char* R;
+    size_t a_batch, b_batch, d_batch, d2_batch, r_batch;
+    uint32_t a_pitch, b_pitch, d_pitch, d2_pitch, r_pitch;
+    int M, N, stages, splits, jobs, batch;
+    float mul;     // accumulator -> the value on D's scale (kEpiQ, kEpiOut: the value itself)
+    float a, b, c; // kEpiQ: b on R's scale
+    float d_scale; // kEpiQ: value -> D's scale
+    // kEpiOut
+    float* out_f32;
+    uint16_t* out_bf16;
+    float* w;
+    const float* lr_dev;
+    float lr, decay, step_scale;
+    int transposed;  // out is N x M
+    float* part;     // kEpiPart: [batch][split][M][N]
+};
+
+// Tiles of one product in bands of four tile rows, columns outside, rows
+// inside: what runs at the same time shares its operand rows in L2.  Below
+// the diagonal only, with SYM.
+template <bool SYM>
+__device__ __forceinline__ void tile_at(int t, int mt, int nt, int& I, int& J)
+{
+    constexpr int GB = 4;
+    if constexpr (!SYM) {
+        const int band = t / (GB * nt);
+        const int h = min(GB, mt - band * GB);
+        const int r = t - band * GB * nt;
+        J = r / h;
+        I = band * GB + r % h;
+    } else {
+        // rows before row i hold i (i + 1) / 2 tiles
+        int band = 0, left = t;
+        for (;;) {
+            const int i0 = band * GB, h = min(GB, mt - i0);
+            const int cnt = h * i0 + h * (h + 1) / 2;
+            if (left < cnt || i0 + h >= mt)
+                break;
+            left -= cnt;
+            ++band;
+        }
+        const int i0 = band * GB, h = min(GB, mt - i0);
+        if (left < h * (i0 + 1)) {
+            J = left / h;
+            I = i0 + left % h;
+        } else {
+            left -= h * (i0 + 1);
+            J = i0 + 1;
+            while (left >= i0 + h - J) {
+                left -= i0 + h - J;
+                ++J;
+            }
+            I = J + left;
+        }
+    }
+}
+
+template <int MI, int NI, int NS, int EPI>
+__global__ void __launch_bounds__(256, (TileNT<OpPair, MI, NI, NS>::kPerCu))
+ns_gemm_kernel(const NsGemm p)
+{
+    typedef TileNT<OpPair, MI, NI, NS> Tile;
+    constexpr bool SYM = EPI == kEpiSym || EPI == kEpiQ || EPI == kEpiPart;
+    static_assert(!SYM || MI == NI, "mirrored tiles are square");
+    const int mt = (p.M + Tile::TM - 1) / Tile::TM;
+    const int nt = (p.N + Tile::TN - 1) / Tile::TN;
+    const int per = SYM ? mt * (mt + 1) / 2 : mt * nt;
+    // consecutive tiles on one XCD (workgroups go round the eight)
+    const int chunk = gridDim.x >> 3;
+    int t = (int)(blockIdx.x & 7) * chunk + (int)(blockIdx.x >> 3);
+    if (t >= per * p.jobs * p.splits * p.batch)
+        return;
+    int I, J;
+    tile_at<SYM>(t % per, mt, nt, I, J);
+    t /= per;
+    const int split = t % p.splits;
+    t /= p.splits;
+    const int job = t % p.jobs, b = t / p.jobs;
+    const int m0 = I * Tile::TM, n0 = J * Tile::TN;
+    const char* A = p.A[job] + b * p.a_batch + (size_t)m0 * p.a_pitch;
+    const char* B = p.B[job] + b * p.b_batch + (size_t)n0 * p.b_pitch;
+    const int s0 = (int)((int64_t)p.stages * split / p.splits);
+    const int s1 = (int)((int64_t)p.stages * (split + 1) / p.splits);
+    floatx16 acc[MI][NI];
+    Tile::run(A, (uint32_t)min(Tile::TM, p.M - m0) * p.a_pitch, p.a_pitch, B,
+              (uint32_t)min(Tile::TN, p.N - n0) * p.b_pitch, p.b_pitch, s0, s1 - s0, acc);
+
+    const int lt = threadIdx.x & 3;
+    if constexpr (EPI == kEpiSym || EPI == kEpiQ) {
+        char* D = p.D[job] + b * p.d_batch;
+        const int kp = (int)(p.d_pitch / 4);
+        const bool mirror = I != J;
+        Tile::each(acc, [&](int di, int dj, float(&v)[4]) {
+            const int i = m0 + di, j = n0 + dj;
+            if constexpr (EPI == kEpiQ) {
+                float r[4] = {0.f, 0.f, 0.f, 0.f};
+                if (j < p.M && i < kp)
+                    load_pair4(p.R + b * p.r_batch, pair_off(p.r_pitch, j, i), r);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] = ((i + e == j && j < p.M ? p.a : 0.f) + p.b * r[e] +
+                            p.c * (v[e] * p.mul)) * p.d_scale;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] *= p.mul;
+            }
+            if (mirror && j < p.M && i < kp)
+                store_pair4(D, pair_off(p.d_pitch, j, i), v);
+            quad_transpose(v);
+            if (i + lt < p.M && j - lt < kp)
+                store_pair4(D, pair_off(p.d_pitch, i + lt, j - lt), v);
+        });
+    } else if constexpr (EPI == kEpiPart) {
+        float* D = p.part + ((size_t)b * p.splits + split) * p.M * p.N;
+        Tile::each(acc, [&](int di, int dj, float(&v)[4]) {
+            const int i = m0 + di, j = n0 + dj;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e < p.M && j < p.N)
+                    D[(size_t)(i + e) * p.N + j] = v[e];
+        });
+    } else if constexpr (EPI == kEpiX) {
+        char *D = p.D[0] + b * p.d_batch, *D2 = p.D2 + b * p.d2_batch;
+        const int kp = (int)(p.d_pitch / 4), kp2 = (int)(p.d2_pitch / 4);
+        Tile::each(acc, [&](int di, int dj, float(&v)[4]) {
+            const int i = m0 + di, j = n0 + dj;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] *= p.mul;
+            if (j < p.N && i < kp2)
+                store_pair4(D2, pair_off(p.d2_pitch, j, i), v);
+            quad_transpose(v);
+            if (i + lt < p.M && j - lt < kp)
+                store_pair4(D, pair_off(p.d_pitch, i + lt, j - lt), v);
+        });
+    } else {
+        const int64_t base = (int64_t)b * p.M * p.N;
+        const float lr = p.w ? (p.lr_dev ? *p.lr_dev : p.lr) : 0.f;
+        Tile::each(acc, [&](int di, int dj, float(&v)[4]) {
+            const int i = m0 + di, j = n0 + dj;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (i + e >= p.M || j >= p.N)
+                    continue;
+                const int64_t at = base + (p.transposed ? (int64_t)j * p.M + i + e
+                                                        : (int64_t)(i + e) * p.N + j);
+                const float o = v[e] * p.mul;
+                if (p.w) {
+                    const float w = p.w[at];
+                    p.w[at] = w - lr * (p.step_scale * o + p.decay * w);
+                } else if (p.out_bf16) {
+                    p.out_bf16[at] = f32_to_bf16_rne(o);
+                } else {
+                    p.out_f32[at] = o;
+                }
+            }
+        });
+    }
+}
+
+// R = sum of the partial products, in order, as a mirrored pair matrix; the
+// parts hold the tiles of 64 below the diagonal.
+__global__ void __launch_bounds__(256)
+ns_reduce_kernel(const float* __restrict__ part, int splits, int m, char* __restrict__ D,
+                 size_t pitch, size_t d_batch, float mul)
+{
+    const int b = blockIdx.z, i = blockIdx.y;
+    const int j = (blockIdx.x * 256 + threadIdx.x) * 4;
+    if (j >= (int)(pitch / 4))
+        return;
+    const float* P = part + (size_t)b * splits * m * m;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (j + e >= m)
+            continue;
+        const size_t at = (j >> 6) <= (i >> 6) ? (size_t)i * m + j + e : (size_t)(j + e) * m + i;
+        for (int s = 0; s < splits; ++s)
+            v[e] += P[(size_t)s * m * m + at];
+        v[e] *= mul;
+    }
+    store_pair4(D + b * d_batch, pair_off(pitch, i, j), v);
+}
+
+// --------------------------------------------------------------------- host
+template <int MI, int NI, int NS, int EPI>
+hipError_t launch_tile(const NsGemm& p, hipStream_t s)
+{
+    constexpr bool SYM = EPI == kEpiSym || EPI == kEpiQ || EPI == kEpiPart;
+    const int64_t mt = (p.M + 64 * MI - 1) / (64 * MI), nt = (p.N + 64 * NI - 1) / (64 * NI);
+    const int64_t tiles =
+        (SYM ? mt * (mt + 1) / 2 : mt * nt) * p.jobs * p.splits * p.batch;
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ns_gemm_kernel<MI, NI, NS, EPI>),
+                       dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+template <int EPI>
+hipError_t launch_gemm(const NsGemm& p, hipStream_t s)
+{
+    return launch_tile<1, 1, 3, EPI>(p, s);
+}
+
+int exponent_for(double bound)  // bound * 2^result <= 2^14
+{
+    int e;
+    frexp(bound, &e);
+    return 14 - e;
+}
+
+}  // namespace
+
+// The ranges of t q(t)^2 and q(t) over t in [0, top]: their extremes lie at
+// the ends or where a derivative vanishes.
+static void ns_ranges(double a, double b, double c, double top, double* qmax, double* tmax)
+{
+    auto q = [&](double t) { return a + b * t + c * t * t; };
+    double at[5] = {0.0, top, 0.0, 0.0, 0.0};
+    int n = 2;
+    if (c != 0.0)
+        at[n++] = -b / (2 * c);
+    // d/dt t q^2 = q (q + 2 t q'):  a + 3 b t + 5 c t^2 = 0 (q = 0 gives the minimum)
+    if (c != 0.0) {
+        const double d = 9 * b * b - 20 * a * c;
+        if (d >= 0) {
+            at[n++] = (-3 * b + sqrt(d)) / (10 * c);
+            at[n++] = (-3 * b - sqrt(d)) / (10 * c);
+        }
+    } else if (b != 0.0) {
+        at[n++] = -a / (3 * b);
+    }
+    *qmax = *tmax = 0.0;
+    for (int i = 0; i < n; ++i)
+        if (at[i] >= 0.0 && at[i] <= top) {
+            *qmax = std::max(*qmax, fabs(q(at[i])));
+            *tmax = std::max(*tmax, at[i] * q(at[i]) * q(at[i]));
+        }
+}
+
+bool ns_plan(int batch, int rows, int cols, int steps, float a, float b, float c, NsPlan* q)
+{
+    *q = NsPlan{};
+    q->batch = batch;
+    q->rows = rows;
+    q->cols = cols;
+    q->tall = rows > cols;
+    q->m = std::min(rows, cols);
+    q->n = std::max(rows, cols);
+    q->steps = steps;
+    // ranges of every step
+    double top = 1.0;
+    q->bound[0] = 1.0;
+    double qall = 0.0;
+    for (int k = 0; k < steps; ++k) {
+        double qmax, tmax;
+        ns_ranges(a, b, c, top, &qmax, &tmax);
+        if (!(tmax <= kNsMaxRange) || !(qmax <= kNsMaxRange))
+            return false;
+        q->qmax[k] = std::max(qmax, 1e-3);
+        q->bound[k + 1] = top = std::max(tmax, 1e-3);
+        qall = std::max(qall, q->qmax[k]);
+    }
+    // the longest first segment, and the longest later one
+    int first = steps, later = steps;
+    if (qall > 1.0) {
+        const double per = 2.0 * log(qall);
+        first = std::min(steps, 1 + (int)floor(log(256.0) / per + 1e-9));
+        later = std::min(steps, 1 + (int)floor(log(16.0) / per + 1e-9));
+    }
+    q->segments = 1 + (steps - first + later - 1) / later;
+    int left = steps;
+    for (int i = q->segments - 1; i > 0; --i) {
+        q->length[i] = std::min(later, left / (i + 1));
+        left -= q->length[i];
+    }
+    q->length[0] = left;
+    const size_t align = 255;
+    const size_t mp = (size_t)((q->m + 31) / 32) * 128, np = (size_t)((q->n + 31) / 32) * 128;
+    q->m_pitch = mp;
+    q->n_pitch = np;
+    q->mm_bytes = ((size_t)q->m * mp + align) & ~align;
+    q->xr_bytes = ((size_t)q->m * np + align) & ~align;
+    q->xt_bytes = ((size_t)q->n * mp + align) & ~align;
+    const int64_t mt = (q->m + 63) / 64, tiles = mt * (mt + 1) / 2 * batch;
+    const int64_t stages = (int64_t)(np / 128);
+    // the Gram product of a short wide matrix has few tiles of long sums: its
+    // reduction is split until the tiles fill the 256 compute units, parts of
+    // at least four stages each
+    q->splits = 1;
+    if (batch > 0 && tiles < 128)
+        q->splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, stages / 4));
+    q->norm_blocks = (int)std::min<int64_t>(kNormBlocks,
+                                            ((int64_t)rows * cols + 4095) / 4096);
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off += (bytes + align) & ~align;
+        return at;
+    };
+    q->off_part = take((size_t)batch * q->norm_blocks * sizeof(double));
+    q->off_split = take(q->splits > 1 ? (size_t)batch * q->splits * q->m * q->m * 4 : 0);
+    q->off_xr = take(batch * q->xr_bytes);
+    q->off_xt[0] = take(batch * q->xt_bytes);
+    q->off_xt[1] = q->segments > 1 ? take(batch * q->xt_bytes) : 0;
+    for (int i = 0; i < 5; ++i)
+        q->off_mm[i] = take(batch * q->mm_bytes);
+    q->ws_bytes = off;
+    return true;
+}
+
+hipError_t launch_newton_schulz(const NsPlan& q, const NsArgs& x, char* ws, hipStream_t s)
+{
+    if (q.batch == 0)
+        return hipSuccess;
+    const int64_t count = (int64_t)q.rows * q.cols;
+    NsInput in{};
+    in.g = x.g;
+    in.v = x.v;
+    in.mu = x.momentum;
+    in.nesterov = x.nesterov;
+    in.bf16 = x.bf16;
+    in.count = count;
+    double* part = (double*)(ws + q.off_part);
+    const dim3 ng((unsigned)q.norm_blocks, (unsigned)q.batch);
+    if (count % 4 == 0)
+        hipLaunchKernelGGL(ns_norm_kernel<4>, ng, dim3(256), 0, s, in, part);
+    else
+        hipLaunchKernelGGL(ns_norm_kernel<1>, ng, dim3(256), 0, s, in, part);
+
+    char *xr = ws + q.off_xr, *xt = ws + q.off_xt[0], *xt2 = ws + q.off_xt[1];
+    int ex = exponent_for(1.0);
+    NsStage st{};
+    st.in = in;
+    st.part = part;
+    st.parts = q.norm_blocks;
+    st.eps = x.eps;
+    st.rows = q.rows;
+    st.cols = q.cols;
+    st.Nl = q.tall ? xt : xr;
+    st.Tl = q.tall ? xr : xt;
+    st.n_pitch = q.tall ? q.m_pitch : q.n_pitch;
+    st.t_pitch = q.tall ? q.n_pitch : q.m_pitch;
+    st.n_batch = q.tall ? q.xt_bytes : q.xr_bytes;
+    st.t_batch = q.tall ? q.xr_bytes : q.xt_bytes;
+    st.scale = ldexpf(1.f, ex);
+    const dim3 sg((unsigned)((q.cols + 63) / 64), (unsigned)((q.rows + 63) / 64),
+                  (unsigned)q.batch);
+    if (q.cols % 4 == 0)
+        hipLaunchKernelGGL(ns_stage_kernel<4>, sg, dim3(256), 0, s, st);
+    else
+        hipLaunchKernelGGL(ns_stage_kernel<1>, sg, dim3(256), 0, s, st);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess)
+        return e;
+
+    auto square = [&](char* A, char* B, char* D) {
+        NsGemm p{};
+        p.A[0] = A;
+        p.B[0] = B;
+        p.D[0] = D;
+        p.a_batch = p.b_batch = p.d_batch = p.r_batch = q.mm_bytes;
+        p.a_pitch = p.b_pitch = p.d_pitch = p.r_pitch = (uint32_t)q.m_pitch;
+        p.M = p.N = q.m;
+        p.stages = (int)(q.m_pitch / 128);
+        p.splits = p.jobs = 1;
+        p.batch = q.batch;
+        return p;
+    };
+    char* R = ws + q.off_mm[0];
+    char* T = ws + q.off_mm[1];
+    char* Qm = ws + q.off_mm[2];
+    int k = 0;
+    for (int seg = 0; seg < q.segments; ++seg) {
+        const int L = q.length[seg];
+        // R = X X^T
+        int er = exponent_for(q.bound[k]);
+        {
+            NsGemm p{};
+            p.A[0] = p.B[0] = xr;
+            p.D[0] = R;
+            p.a_batch = p.b_batch = q.xr_bytes;
+            p.d_batch = q.mm_bytes;
+            p.a_pitch = p.b_pitch = (uint32_t)q.n_pitch;
+            p.d_pitch = (uint32_t)q.m_pitch;
+            p.M = p.N = q.m;
+            p.stages = (int)(q.n_pitch / 128);
+            p.splits = q.splits;
+            p.jobs = 1;
+            p.batch = q.batch;
+            p.mul = ldexpf(1.f, er - 2 * ex);
+            if (q.splits > 1) {
+                p.part = (float*)(ws + q.off_split);
+                e = launch_tile<1, 1, 3, kEpiPart>(p, s);
+                if (e != hipSuccess)
+                    return e;
+                hipLaunchKernelGGL(ns_reduce_kernel,
+                                   dim3((unsigned)((q.m_pitch / 4 + 1023) / 1024), (unsigned)q.m,
+                                        (unsigned)q.batch),
+                                   dim3(256), 0, s, p.part, q.splits, q.m, R, q.m_pitch,
+                                   q.mm_bytes, p.mul);
+                e = hipGetLastError();
+            } else {
+                e = launch_gemm<kEpiSym>(p, s);
+            }
+            if (e != hipSuccess)
+                return e;
+        }
+        char* P = nullptr;
+        int ep = 0;
+        double pbound = 1.0;
+        for (int l = 0; l < L; ++l, ++k) {
+            // Q = a I + b R + c R R; the segment's first is its P as well
+            char* spare = ws + q.off_mm[P == ws + q.off_mm[3] ? 4 : 3];
+            char* Q = P ? Qm : spare;
+            const int eq = exponent_for(q.qmax[k]);
+            NsGemm p = square(R, R, Q);
+            p.R = R;
+            p.mul = ldexpf(1.f, -2 * er);
+            p.a = x.a;
+            p.b = ldexpf(x.b, -er);
+            p.c = x.c;
+            p.d_scale = ldexpf(1.f, eq);
+            if ((e = launch_gemm<kEpiQ>(p, s)) != hipSuccess)
+                return e;
+            pbound *= q.qmax[k];
+            const bool more = l + 1 < L;
+            const int et = exponent_for(q.qmax[k] * q.bound[k]);
+            const int ep2 = exponent_for(pbound);
+            char* P2 = spare;
+            if (more) {
+                p = square(Q, R, T);
+                p.mul = ldexpf(1.f, et - eq - er);
+                if ((e = launch_gemm<kEpiSym>(p, s)) != hipSuccess)
+                    return e;
+            }
+            if (P) {
+                p = square(Q, P, P2);
+                p.mul = ldexpf(1.f, ep2 - eq - ep);
+                if ((e = launch_gemm<kEpiSym>(p, s)) != hipSuccess)
+                    return e;
+            }
+            if (more) {
+                er = exponent_for(q.bound[k + 1]);
+                p = square(T, Q, R);
+                p.mul = ldexpf(1.f, er - et - eq);
+                if ((e = launch_gemm<kEpiSym>(p, s)) != hipSuccess)
+                    return e;
+            }
+            P = P2;
+            ep = P == Q ? eq : ep2;
+        }
+        // X = P X
+        NsGemm p{};
+        p.A[0] = P;
+        p.B[0] = xt;
+        p.a_batch = q.mm_bytes;
+        p.b_batch = q.xt_bytes;
+        p.a_pitch = p.b_pitch = (uint32_t)q.m_pitch;
+        p.M = q.m;
+        p.N = q.n;
+        p.stages = (int)(q.m_pitch / 128);
+        p.splits = p.jobs = 1;
+        p.batch = q.batch;
+        if (seg + 1 < q.segments) {
+            const int ex2 = exponent_for(sqrt(q.bound[k]));
+            p.D[0] = xr;
+            p.D2 = xt2;
+            p.d_batch = q.xr_bytes;
+            p.d2_batch = q.xt_bytes;
+            p.d_pitch = (uint32_t)q.n_pitch;
+            p.d2_pitch = (uint32_t)q.m_pitch;
+            p.mul = ldexpf(1.f, ex2 - ep - ex);
+            ex = ex2;
+            std::swap(xt, xt2);
+            e = launch_gemm<kEpiX>(p, s);
+        } else {
+            p.mul = ldexpf(1.f, -ep - ex);
+            p.out_f32 = (float*)x.out;
+            p.out_bf16 = x.bf16 ? (uint16_t*)x.out : nullptr;
+            p.w = x.w;
+            p.lr = x.lr;
+            p.lr_dev = x.lr_dev;
+            p.decay = x.decay;
+            p.step_scale = x.step_scale;
+            p.transposed = q.tall;
+            e = launch_gemm<kEpiOut>(p, s);
+        }
+        if (e != hipSuccess)
+            return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace caffe_hip

@@ -1,0 +1,187 @@
+"""Orthogonalised updates, 8-bit rows and their inner product on the CPU: every
+invalid argument becomes its status code before any GPU work, and the
+workspace queries answer without a GPU."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_1408_5093_amd as cc
+
+P = ctypes.c_void_p
+INVALID, ALIGN, WORKSPACE, UNSUPPORTED = -1, -2, -3, -4
+
+
+def _ns(**kw):
+    d = cc.ns_desc((2, 20, 30))
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("batch", -1, INVALID), ("rows", 0, INVALID), ("cols", 0, INVALID), ("steps", 0, INVALID),
+    ("eps", -1.0, INVALID), ("eps", float("nan"), INVALID), ("a", float("inf"), INVALID),
+    ("b", float("nan"), INVALID), ("rows", (1 << 20) + 1, UNSUPPORTED),
+    ("cols", (1 << 20) + 1, UNSUPPORTED), ("steps", 65, UNSUPPORTED), ("dtype", 2, UNSUPPORTED),
+    ("dtype", 9, UNSUPPORTED), ("batch", 65536, UNSUPPORTED),
+    ("a", 40.0, UNSUPPORTED),  # singular values grow without bound
+])
+def test_newton_schulz_descriptor(field, value, code):
+    lib = cc.load()
+    d = _ns(**{field: value})
+    n = ctypes.c_size_t()
+    assert lib.caffe_newton_schulz_workspace_size(ctypes.byref(d), ctypes.byref(n)) == code
+    assert lib.caffe_newton_schulz(ctypes.byref(d), P(0x1000), P(0x2000), P(0x10000), 1 << 40,
+                                   None) == code
+    assert lib.caffe_muon_update(ctypes.byref(d), P(0x1000), P(0x2000), P(0x3000), 0.1, 0.9, 0.0,
+                                 1.0, 1, P(0x10000), 1 << 40, None) == code
+    assert lib.caffe_last_error() != b""
+
+
+def test_newton_schulz_pointers_and_workspace():
+    lib = cc.load()
+    d = _ns()
+    need = cc.newton_schulz_workspace_size(d)
+    assert need > 0
+
+    def call(i=0x1000, o=0x2000, ws=0x10000, n=need):
+        return lib.caffe_newton_schulz(ctypes.byref(d), P(i), P(o), P(ws), n, None)
+
+    assert call(i=None) == INVALID and call(o=None) == INVALID
+    assert call(i=0x1008) == ALIGN and call(o=0x2004) == ALIGN
+    assert call(ws=None) in (INVALID, WORKSPACE) and call(ws=0x10010) == ALIGN
+    assert call(n=need - 1) == WORKSPACE
+    n = ctypes.c_size_t()
+    assert lib.caffe_newton_schulz_workspace_size(None, ctypes.byref(n)) == INVALID
+    assert lib.caffe_newton_schulz_workspace_size(ctypes.byref(d), None) == INVALID
+
+
+def test_muon_update_arguments():
+    lib = cc.load()
+    d = _ns()
+    need = cc.newton_schulz_workspace_size(d)
+    nan = float("nan")
+
+    def call(w=0x1000, g=0x2000, v=0x3000, lr=0.1, mu=0.9, wd=0.0, sc=1.0, nest=1, n=need, d=d):
+        return lib.caffe_muon_update(ctypes.byref(d), P(w), P(g), P(v), lr, mu, wd, sc, nest,
+                                     P(0x10000), n, None)
+
+    for kw in (dict(lr=nan), dict(mu=nan), dict(wd=nan), dict(sc=nan), dict(nest=2),
+               dict(w=None), dict(g=None), dict(v=None)):
+        assert call(**kw) == INVALID, kw
+    assert call(w=0x1004) == ALIGN and call(n=need - 1) == WORKSPACE
+    assert call(d=_ns(dtype=cc.CAFFE_BF16)) == UNSUPPORTED
+
+    def dev(lr):
+        return lib.caffe_muon_update_device_lr(ctypes.byref(d), P(0x1000), P(0x2000), P(0x3000),
+                                               P(lr), 0.9, 0.0, 1.0, 1, P(0x10000), 0, None)
+
+    assert dev(None) == INVALID and dev(0x1002) == ALIGN and dev(0x1004) == WORKSPACE
+
+
+def test_empty_batches_need_no_gpu():
+    lib = cc.load()
+    d = _ns(batch=0)
+    assert lib.caffe_newton_schulz(ctypes.byref(d), None, None, P(0x10000), 1 << 30, None) == 0
+    assert lib.caffe_quantize_rows(None, 0, 0, 10, None, None, None) == 0
+    d = cc.Ip8Desc(0, 10, 5, 0, cc.CAFFE_F32, cc.CAFFE_F32)
+    assert lib.caffe_inner_product_int8(ctypes.byref(d), None, None, None, None, None, None, None,
+                                        0, None) == 0
+
+
+def test_coefficients_that_stay_in_range():
+    for coef, steps in (((1.5, -0.5, 0.0), 30), ((3.4445, -4.7750, 2.0315), 10),
+                        ((15 / 8, -10 / 8, 3 / 8), 20), ((1.0, 0.0, 0.0), 64)):
+        assert cc.newton_schulz_workspace_size(cc.ns_desc((64, 64), steps, coef)) > 0
+    for coef, steps in (((2.0, 0.0, 0.0), 20), ((3.0, 5.0, 1.0), 5)):
+        with pytest.raises(cc.CaffeError, match="range"):
+            cc.newton_schulz_workspace_size(cc.ns_desc((64, 64), steps, coef))
+
+
+def test_ns_desc_shapes():
+    d = cc.ns_desc((384, 192, 3, 3), group=2)
+    assert (d.batch, d.rows, d.cols) == (2, 192, 1728)
+    d = cc.ns_desc((5, 7, 9))
+    assert (d.batch, d.rows, d.cols) == (5, 7, 9)
+    for shape, g in (((5,), 1), ((4, 3, 2), 2), ((5, 4), 2), ((5, 4), 0)):
+        with pytest.raises(ValueError):
+            cc.ns_desc(shape, group=g)
+
+
+def test_int8_pitch():
+    lib = cc.load()
+    for cols, pitch in ((1, 128), (128, 128), (129, 256), (9216, 9216), (1 << 17, 1 << 17)):
+        assert cc.int8_pitch(cols) == pitch
+    for cols in (0, -5, (1 << 17) + 1):
+        assert lib.caffe_int8_pitch(cols) == 0
+        with pytest.raises(ValueError):
+            cc.int8_pitch(cols)
+
+
+@pytest.mark.parametrize("args,code", [
+    ((0x1000, 0, -1, 10, 0x2000, 0x3000), INVALID), ((0x1000, 0, 3, 0, 0x2000, 0x3000), INVALID),
+    ((0x1000, 2, 3, 10, 0x2000, 0x3000), UNSUPPORTED),
+    ((0x1000, 0, 3, (1 << 17) + 1, 0x2000, 0x3000), UNSUPPORTED),
+    ((0x1000, 0, 1 << 31, 10, 0x2000, 0x3000), UNSUPPORTED),
+    ((None, 0, 3, 10, 0x2000, 0x3000), INVALID), ((0x1000, 0, 3, 10, None, 0x3000), INVALID),
+    ((0x1000, 0, 3, 10, 0x2000, None), INVALID), ((0x1004, 0, 3, 10, 0x2000, 0x3000), ALIGN),
+    ((0x1000, 0, 3, 10, 0x2008, 0x3000), ALIGN), ((0x1000, 0, 3, 10, 0x2000, 0x3004), ALIGN),
+])
+def test_quantize_rows_arguments(args, code):
+    x, dt, rows, cols, q, s = args
+    assert cc.load().caffe_quantize_rows(P(x), dt, rows, cols, P(q), P(s), None) == code
+
+
+def _ip8(**kw):
+    d = cc.Ip8Desc(3, 100, 7, 0, cc.CAFFE_F32, cc.CAFFE_F32)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("N", -1, INVALID), ("C", 0, INVALID), ("K", 0, INVALID), ("relu", 2, INVALID),
+    ("bottom_type", 2, UNSUPPORTED), ("top_type", 16, UNSUPPORTED),
+    ("C", (1 << 17) + 1, UNSUPPORTED), ("N", 1 << 30, UNSUPPORTED),
+])
+def test_inner_product_int8_descriptor(field, value, code):
+    lib = cc.load()
+    d = _ip8(**{field: value})
+    if field == "N" and value > 0:
+        d.K = 1 << 20
+    n = ctypes.c_size_t()
+    assert lib.caffe_inner_product_int8_workspace_size(ctypes.byref(d), ctypes.byref(n)) == code
+    assert lib.caffe_inner_product_int8(ctypes.byref(d), P(0x1000), None, P(0x2000), P(0x3000),
+                                        None, P(0x4000), P(0x10000), 1 << 40, None) == code
+
+
+def test_inner_product_int8_pointers():
+    lib = cc.load()
+
+    def call(d=None, x=0x1000, xs=None, w=0x2000, t=0x3000, b=None, top=0x4000, ws=0x10000, n=1 << 20):
+        return lib.caffe_inner_product_int8(ctypes.byref(d or _ip8()), P(x), P(xs), P(w), P(t),
+                                            P(b), P(top), P(ws), n, None)
+
+    for kw in (dict(x=None), dict(w=None), dict(t=None), dict(top=None), dict(xs=0x5000),
+               dict(d=_ip8(bottom_type=cc.CAFFE_INT8_ROWS))):
+        assert call(**kw) == INVALID, kw
+    for kw in (dict(x=0x1004), dict(w=0x2008), dict(t=0x3004), dict(b=0x5004), dict(top=0x4008),
+               dict(ws=0x10080)):
+        assert call(**kw) == ALIGN, kw
+    assert call(n=3 * 128 + 11) == WORKSPACE
+    n = ctypes.c_size_t()
+    d = _ip8(bottom_type=cc.CAFFE_INT8_ROWS)
+    assert lib.caffe_inner_product_int8_workspace_size(ctypes.byref(d), ctypes.byref(n)) == 0
+    assert n.value == 0
+
+
+def test_host_tensors_and_shapes_are_refused():
+    x = torch.zeros(4, 8)
+    for f in (lambda: cc.newton_schulz(x), lambda: cc.muon_update(x, x.clone(), x.clone(), 0.1),
+              lambda: cc.quantize_rows(x), lambda: cc.newton_schulz(x.double()),
+              lambda: cc.quantize_rows(x.half()),
+              lambda: cc.inner_product_int8(x, torch.zeros(3, 128, dtype=torch.int8),
+                                            torch.zeros(3))):
+        with pytest.raises(ValueError):
+            f()

@@ -1,0 +1,240 @@
+"""8-bit rows and their inner product against whole-number arithmetic on the
+CPU.  The rows have to be equal: the scale is one float division, the rounding
+of each quotient exact.  The product's sum is exact, so a float result has the
+roundings of (sum * s) * t + bias: the sum to float, two products and the
+addition, four of 2^-24 of |sum s t| + |bias| (TOL = 2^-22 of that); a
+bfloat16 result adds 2^-8 of itself.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_1408_5093_amd as cc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+TOL, TOL_BF16 = 2.0 ** -22, 2.0 ** -8
+
+
+def dev(a, dtype=torch.float32):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV, dtype)
+
+
+def rows_ref(x):
+    """(q, scale) of float32 rows."""
+    x = np.asarray(x, dtype=np.float32)
+    amax = np.abs(x).max(1)
+    with np.errstate(all="ignore"):
+        s = (amax.astype(np.float64) / 127).astype(np.float32)
+        t = x.astype(np.float64) / s.astype(np.float64)[:, None]
+    # a quotient of two floats that is not on a half is 2^-48 of itself away or
+    # more, and double's is 2^-53 off: rint of it is exact
+    bad = ~np.isfinite(x).all(1)
+    q = np.clip(np.rint(np.where((s > 0)[:, None] & ~bad[:, None], t, 0)), -127, 127)
+    s = np.where(bad, np.float32("nan"), s)
+    return q.astype(np.int8), s.astype(np.float32)
+
+
+def check_rows(q, s, x):
+    q, s = q.cpu().numpy(), s.cpu().numpy()
+    q_ref, s_ref = rows_ref(x)
+    cols = x.shape[1]
+    np.testing.assert_array_equal(s, s_ref)
+    np.testing.assert_array_equal(q[:, :cols], q_ref)
+    assert (q[:, cols:] == 0).all()
+
+
+@pytest.mark.parametrize("rows", [1, 5, 130])
+@pytest.mark.parametrize("cols", [1, 3, 4, 127, 128, 129, 1000, 1023, 1024, 1025, 1028, 4096, 4097,
+                                  4100, 9216, 16383, 16384, 16385, 20000])
+def test_quantize_rows(rows, cols):
+    print(f"quantize {rows}x{cols}", flush=True)
+    rng = np.random.default_rng([20, rows, cols])
+    x = (rng.standard_normal((rows, cols)) * np.exp(rng.uniform(-9, 9, (rows, 1)))).astype(
+        np.float32)
+    check_rows(*cc.quantize_rows(dev(x)), x)
+    xb = dev(x, torch.bfloat16)
+    check_rows(*cc.quantize_rows(xb), xb.float().cpu().numpy())
+
+
+def test_quantize_longest_rows():
+    x = np.random.default_rng(21).standard_normal((3, 1 << 17)).astype(np.float32)
+    check_rows(*cc.quantize_rows(dev(x)), x)
+
+
+def test_quantize_rows_at_halves():
+    """Quotients on a half, and the floats next to them, to the even number and
+    to their own side."""
+    rng = np.random.default_rng(22)
+    rows = []
+    for s in np.concatenate([[1.0, 0.5, 2.0 ** -20, 3.0, 1e-3, 1e30],
+                             np.exp(rng.uniform(-20, 20, 200))]).astype(np.float32):
+        top = np.float32(127) * s  # exact or not: the scale is what the reference says
+        k = np.arange(-126, 126, dtype=np.float64) + 0.5
+        x = (k * float(np.float32(float(top) / 127))).astype(np.float32)
+        rows.append(np.concatenate([[top], x, np.nextafter(x, np.float32(np.inf)),
+                                    np.nextafter(x, np.float32(-np.inf))]))
+    x = np.stack(rows).astype(np.float32)
+    check_rows(*cc.quantize_rows(dev(x)), x)
+
+
+def test_quantize_rows_special_values():
+    x = np.zeros((9, 300), np.float32)
+    x[1, 7], x[2, 299], x[3, 0] = np.nan, np.inf, -np.inf
+    x[4, 5] = 1e-45           # the scale vanishes
+    x[5] = 3e-38 * np.linspace(-1, 1, 300)  # subnormal scale
+    x[6] = -2.0
+    x[7] = np.float32(3.4e38) * np.linspace(-1, 1, 300).astype(np.float32)
+    x[8, 1] = -0.0
+    q, s = cc.quantize_rows(dev(x))
+    check_rows(q, s, x)
+    assert np.isnan(s.cpu().numpy()[1:4]).all() and (q[1:4] == 0).all()
+    assert s[0] == 0 and s[4] == 0 and s[8] == 0
+
+
+def test_quantize_rows_past_2_31_bytes():
+    rows, cols = 150000, 8192
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 16 GB of device memory")
+    print("quantize 150000x8192", flush=True)
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device=DEV)
+    tail = np.random.default_rng(23).standard_normal((3, cols)).astype(np.float32)
+    x[-3:] = dev(tail)
+    q, s = cc.quantize_rows(x)
+    check_rows(q[-3:], s[-3:], x[-3:].float().cpu().numpy())
+    assert int(torch.count_nonzero(s)) == 3
+    w, ws = cc.quantize_rows(dev(tail))
+    y = cc.inner_product_int8(q, w, ws, C=cols, x_scale=s)
+    ref = ip_ref(q[-3:].cpu().numpy(), s[-3:].cpu().numpy(), w.cpu().numpy(), ws.cpu().numpy(),
+                 None, False)
+    check_top(y[-3:], *ref)
+    assert int(torch.count_nonzero(y[:-3])) == 0
+
+
+def ip_ref(q, s, p, t, bias, relu):
+    """(top, the sum of its terms' sizes)."""
+    z = (q.astype(np.int64) @ p.astype(np.int64).T).astype(np.float64)
+    z = z * s.astype(np.float64)[:, None] * t.astype(np.float64)[None, :]
+    size = np.abs(z) + (0 if bias is None else np.abs(bias))
+    z = z if bias is None else z + bias
+    return (np.maximum(z, 0) if relu else z), size
+
+
+def check_top(top, ref, size):
+    got = top.double().cpu().numpy()
+    assert got.shape == ref.shape
+    tol = TOL * size + (TOL_BF16 * np.abs(ref) if top.dtype == torch.bfloat16 else 0)
+    assert (np.abs(got - ref) <= tol).all(), float((np.abs(got - ref) - tol).max())
+
+
+PRODUCTS = [(1, 1, 1), (1, 9216, 4096), (1, 100, 10), (2, 129, 65), (3, 1003, 507), (4, 500, 1000),
+            (5, 128, 64), (7, 4096, 130), (8, 333, 77), (9, 333, 77), (15, 2000, 300),
+            (16, 256, 1000), (17, 640, 129), (33, 1003, 507), (63, 64, 63), (64, 800, 500),
+            (65, 127, 200), (130, 5000, 70), (256, 1024, 1000), (300, 400, 513), (700, 96, 1200)]
+
+
+@pytest.mark.parametrize("N,C,K", PRODUCTS)
+@pytest.mark.parametrize("bottom,top,relu,bias", [
+    (torch.float32, torch.float32, True, True), (torch.bfloat16, torch.bfloat16, False, True),
+    (torch.int8, torch.float32, False, False), (torch.int8, torch.bfloat16, True, True)])
+def test_inner_product(N, C, K, bottom, top, relu, bias):
+    print(f"int8 product N={N} C={C} K={K} {bottom} {top}", flush=True)
+    rng = np.random.default_rng([24, N, C, K])
+    w = (rng.standard_normal((K, C)) * 0.01).astype(np.float32)
+    x = np.maximum(rng.standard_normal((N, C)), 0).astype(np.float32)
+    b = rng.standard_normal(K).astype(np.float32) if bias else None
+    wq, wsc = cc.quantize_rows(dev(w))
+    p, t = wq.cpu().numpy(), wsc.cpu().numpy()
+    bt = dev(b) if bias else None
+    if bottom == torch.int8:
+        xt, xs = cc.quantize_rows(dev(x))
+        q, s = xt.cpu().numpy(), xs.cpu().numpy()
+        y = cc.inner_product_int8(xt, wq, wsc, bt, C=C, x_scale=xs, relu=relu, top_dtype=top)
+    else:
+        xt = dev(x, bottom)
+        q, s = rows_ref(xt.float().cpu().numpy())
+        p = p[:, :C]
+        y = cc.inner_product_int8(xt, wq, wsc, bt, relu=relu, top_dtype=top)
+    assert y.dtype == top
+    check_top(y, *ip_ref(q, s, p, t, b, relu))
+
+
+@pytest.mark.parametrize("N", [1, 6, 40, 200])
+def test_inner_product_extreme_sums(N):
+    """The longest rows, all at +-127: sums up to 127^2 2^17 < 2^31."""
+    C, K = 1 << 17, 70
+    xq = torch.full((N, C), 127, dtype=torch.int8, device=DEV)
+    wq = torch.full((K, C), 127, dtype=torch.int8, device=DEV)
+    wq[1::2] = -127
+    one = lambda n: torch.full((n,), 2.0 ** -10, device=DEV)  # noqa: E731
+    y = cc.inner_product_int8(xq, wq, one(K), C=C, x_scale=one(N))
+    sign = np.where(np.arange(K) % 2, -1.0, 1.0)
+    ref = np.broadcast_to(sign * (127.0 ** 2 * C * 2.0 ** -20), (N, K))
+    check_top(y, ref, np.abs(ref))
+
+
+@pytest.mark.parametrize("N", [1, 3, 20, 100])
+def test_inner_product_rows_that_hold_nothing(N):
+    """A zero sample gives the bias, one with a NaN or an infinity NaN (0 with
+    relu, as in the convolution layer); the others are as without them."""
+    rng = np.random.default_rng(25)
+    C, K = 200, 90
+    x = rng.standard_normal((N + 3, C)).astype(np.float32)
+    x[0], x[1, 5], x[2, 199] = 0, np.nan, -np.inf
+    wq, ws = cc.quantize_rows(dev(rng.standard_normal((K, C))))
+    b = dev(rng.standard_normal(K))
+    y = cc.inner_product_int8(dev(x), wq, ws, b)
+    assert torch.equal(y[0], b) and torch.isnan(y[1:3]).all()
+    z = cc.inner_product_int8(dev(x), wq, ws, b, relu=True)
+    assert (z[1:3] == 0).all() and torch.equal(z[0], b.clamp(min=0))
+    check_top(y[3:], *ip_ref(*rows_ref(x[3:]), wq.cpu().numpy()[:, :C], ws.cpu().numpy(),
+                             b.cpu().numpy(), False))
+
+
+@pytest.mark.parametrize("N", [1, 40])
+def test_inner_product_captured_and_on_another_stream(N):
+    rng = np.random.default_rng(26)
+    C, K = 700, 300
+    xs = [dev(rng.standard_normal((N, C))) for _ in range(3)]
+    wq, wsc = cc.quantize_rows(dev(rng.standard_normal((K, C))))
+    x, out, ws = xs[0].clone(), torch.empty((N, K), device=DEV), cc.Workspace()
+    cc.inner_product_int8(x, wq, wsc, out=out, ws=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cc.inner_product_int8(x, wq, wsc, out=out, ws=ws)
+    for a in xs:
+        x.copy_(a)
+        graph.replay()
+        eager = cc.inner_product_int8(a, wq, wsc)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        y = cc.inner_product_int8(xs[2], wq, wsc)
+    s.synchronize()
+    assert torch.equal(y, out)
+
+
+def test_refusals():
+    x = torch.zeros(3, 100, device=DEV)
+    w, t = torch.zeros(5, 128, dtype=torch.int8, device=DEV), torch.zeros(5, device=DEV)
+    q = torch.zeros(3, 128, dtype=torch.int8, device=DEV)
+    for kw, match in ((dict(x=q, weight=w, weight_scale=t), "C"),
+                      (dict(x=q, weight=w, weight_scale=t, C=100), "x_scale"),
+                      (dict(x=x, weight=w, weight_scale=t, x_scale=t), "x_scale"),
+                      (dict(x=x, weight=w, weight_scale=t[:4]), "K="),
+                      (dict(x=x, weight=w, weight_scale=t, bias=t[:4]), "K="),
+                      (dict(x=x, weight=w, weight_scale=t, C=90), "rows of C"),
+                      (dict(x=x, weight=w[:, :64], weight_scale=t), "contiguous"),
+                      (dict(x=x.half(), weight=w, weight_scale=t), "bottom"),
+                      (dict(x=x, weight=w, weight_scale=t, top_dtype=torch.float16), "top"),
+                      (dict(x=x, weight=w, weight_scale=t, out=torch.empty(3, 4, device=DEV)),
+                       "elements")):
+        with pytest.raises(ValueError, match=match):
+            cc.inner_product_int8(**kw)
+    with pytest.raises(ValueError):
+        cc.quantize_rows(x[0])
+    with pytest.raises(ValueError):
+        cc.quantize_rows(x, q=q[:, :100])

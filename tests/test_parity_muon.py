@@ -1,0 +1,250 @@
+"""Newton-Schulz orthogonalisation and the update along it, against the
+definitions in 64 bits (step by step, on the CPU).
+
+Tolerance, in the 2-norm relative to the result's.  The operands hold 22 bits
+(two half terms), a rounding error of at most 2^-23 of an element, and float
+sums add 2^-24 of a partial sum at a time; in one product of unit operands
+these make an error of at most about 2^-20 in the largest singular direction.
+A segment lets errors of the Gram matrix grow at most 2^8 against a value that
+stays below 1, so the worst direction of the worst matrix ends near
+2^-20 * 2^8 = 2.4e-4 (HARD: matrices with singular values near zero in few
+dimensions).  Where m directions share the rounding errors, they are
+independent and each takes 1/sqrt(m) of them or less: 2^-16 (TOL, 1.5e-5) for
+gradient-like matrices.  A bfloat16 result adds its own rounding, 2^-8 at the
+most (TOL_BF16 = 2^-8 + TOL).
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_1408_5093_amd as cc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+TOL, HARD = 2.0 ** -16, 2.0 ** -12
+TOL_BF16 = 2.0 ** -8 + TOL
+CUBIC = (1.5, -0.5, 0.0)
+
+
+def ns_ref(g, steps, coef=cc.NS_COEF, eps=1e-7):
+    a, b, c = (float(np.float32(v)) for v in coef)
+    out = []
+    for x in np.asarray(g, dtype=np.float64):
+        tall = x.shape[0] > x.shape[1]
+        x = x.T if tall else x
+        n = np.sqrt((x * x).sum())
+        x = x / (n + float(np.float32(eps))) if n else x
+        for _ in range(steps):
+            A = x @ x.T
+            x = a * x + (b * A + c * (A @ A)) @ x
+        out.append(x.T if tall else x)
+    return np.stack(out)
+
+
+def gradient(rng, batch, rows, cols, rank=8, noise=0.2):
+    d = rng.standard_normal((batch, rows, rank))
+    x = np.maximum(rng.standard_normal((batch, rank, cols)), 0)
+    return ((d @ x / rank + noise * rng.standard_normal((batch, rows, cols))) * 1e-3).astype(
+        np.float32)
+
+
+def rel(got, ref):
+    got = got.double().cpu().numpy() if isinstance(got, torch.Tensor) else got
+    assert got.shape == ref.shape
+    assert np.isfinite(got).all()
+    return float(np.linalg.norm(got - ref) / max(np.linalg.norm(ref), 1e-300))
+
+
+def dev(a, dtype=torch.float32):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV, dtype)
+
+
+SIZES = [(1, 1, 1), (1, 1, 7), (1, 5000, 1), (2, 3, 5), (1, 20, 25), (3, 31, 33), (1, 50, 500),
+         (3, 64, 64), (1, 65, 63), (1, 127, 513), (1, 1000, 33), (1, 128, 128), (1, 129, 65),
+         (2, 129, 1000), (2, 192, 1728), (1, 130, 4100), (1, 257, 300), (4, 200, 210),
+         (1, 500, 800), (1, 900, 640), (1, 16, 40000)]
+
+
+@pytest.mark.parametrize("batch,rows,cols", SIZES)
+def test_newton_schulz_float(batch, rows, cols):
+    print(f"newton_schulz {batch}x{rows}x{cols}", flush=True)
+    g = gradient(np.random.default_rng([1, batch, rows, cols]), batch, rows, cols)
+    ref = ns_ref(g, 5)
+    x = dev(g)
+    assert rel(cc.newton_schulz(x), ref) <= TOL
+    assert np.array_equal(x.cpu().numpy(), g)  # the input is left as it was
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(1, 1, 9), (2, 50, 500), (1, 605, 603), (1, 1111, 300),
+                                             (3, 100, 77), (1, 33, 130)])
+def test_newton_schulz_bf16(batch, rows, cols):
+    print(f"newton_schulz bf16 {batch}x{rows}x{cols}", flush=True)
+    x = dev(gradient(np.random.default_rng([2, batch, rows, cols]), batch, rows, cols),
+            torch.bfloat16)
+    out = cc.newton_schulz(x)
+    assert out.dtype == torch.bfloat16
+    assert rel(out, ns_ref(x.double().cpu().numpy(), 5)) <= TOL_BF16
+
+
+@pytest.mark.parametrize("coef,steps", [(cc.NS_COEF, 1), (cc.NS_COEF, 2), (cc.NS_COEF, 3),
+                                        (cc.NS_COEF, 4), (cc.NS_COEF, 6), (cc.NS_COEF, 10),
+                                        (CUBIC, 1), (CUBIC, 7), (CUBIC, 16),
+                                        ((15 / 8, -10 / 8, 3 / 8), 9)])
+@pytest.mark.parametrize("shape", [(2, 40, 90), (1, 150, 200)])
+def test_newton_schulz_steps_and_coefficients(coef, steps, shape):
+    print(f"newton_schulz {shape} {coef} x {steps}", flush=True)
+    g = gradient(np.random.default_rng([3, steps]), *shape)
+    assert rel(cc.newton_schulz(dev(g), steps, coef), ns_ref(g, steps, coef)) <= TOL
+
+
+@pytest.mark.parametrize("n", [3, 40, 100, 160, 300])
+def test_newton_schulz_hard_matrices(n):
+    """Singular values that vanish or span nine decades, equal rows, an
+    orthogonal matrix, a lower-triangular one."""
+    rng = np.random.default_rng([4, n])
+    q, _ = np.linalg.qr(rng.standard_normal((n, n)))
+    u, _ = np.linalg.qr(rng.standard_normal((n, n)))
+    mats = {"rank one": np.outer(rng.standard_normal(n), rng.standard_normal(n)),
+            "orthogonal": q, "decades": (q * np.logspace(0, -9, n)) @ u,
+            "equal rows": np.tile(rng.standard_normal(n), (n, 1)),
+            "triangular": np.tril(rng.standard_normal((n, n)))}
+    for name, g in mats.items():
+        print(f"hard {n}: {name}", flush=True)
+        g = g.astype(np.float32)[None]
+        assert rel(cc.newton_schulz(dev(g)), ns_ref(g, 5)) <= HARD, name
+
+
+def test_newton_schulz_scale_of_the_input():
+    """The norm is taken in double: no scale of the floats over- or underflows
+    it, and eps counts as it is defined (a norm far below eps leaves nothing:
+    the operands' absolute accuracy is 2^-39)."""
+    g = gradient(np.random.default_rng(5), 1, 60, 90)
+    for s in (1e-30, 1e-8, 1.0, 1e20, 1e38):
+        x = (g / np.abs(g).max() * np.float32(s)).astype(np.float32)
+        if s > 1e-10:
+            assert rel(cc.newton_schulz(dev(x)), ns_ref(x, 5)) <= TOL, s
+        # at eps = 0 the direction alone counts
+        assert rel(cc.newton_schulz(dev(x), eps=0.0), ns_ref(x, 5, eps=0.0)) <= TOL, s
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 70), (200, 260)])
+def test_newton_schulz_zero_and_not_finite(rows, cols):
+    """A zero matrix gives zeros, one with a NaN or infinity NaN everywhere; the
+    others of the batch are as without them."""
+    g = gradient(np.random.default_rng(6), 5, rows, cols)
+    alone = cc.newton_schulz(dev(g))
+    g[1] = 0
+    g[2, 3, 4] = np.nan
+    g[3, rows - 1, cols - 1] = np.inf
+    for eps in (1e-7, 0.0):
+        out = cc.newton_schulz(dev(g), eps=eps)
+        assert (out[1] == 0).all()
+        assert torch.isnan(out[2]).all() and torch.isnan(out[3]).all()
+        if eps:
+            assert torch.equal(out[0], alone[0]) and torch.equal(out[4], alone[4])
+
+
+@pytest.mark.parametrize("rows,cols", [(60, 90), (300, 170)])
+def test_newton_schulz_in_place_any_workspace_any_stream(rows, cols):
+    """The same bits in place, on a workspace full of NaN, and on another
+    stream."""
+    g = gradient(np.random.default_rng(7), 2, rows, cols)
+    first = cc.newton_schulz(dev(g))
+    ws = cc.Workspace()
+    ws.get(cc.newton_schulz_workspace_size(cc.ns_desc(g.shape))).fill_(255)
+    x = dev(g)
+    assert torch.equal(cc.newton_schulz(x, out=x, ws=ws), first)
+    x = dev(g)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    out = torch.empty_like(x)
+    with torch.cuda.stream(s):
+        cc.newton_schulz(x, out=out)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(out, first)
+    out = torch.empty_like(x)
+    torch.cuda.synchronize()
+    cc.newton_schulz(x, out=out, stream=s, ws=ws)
+    torch.cuda.synchronize()
+    assert torch.equal(out, first)
+
+
+def muon_ref(w, g, v, lr, mu, wd, nesterov, scale, steps=5):
+    f = lambda t: float(np.float32(t))  # noqa: E731
+    w, g, v = (np.asarray(t, dtype=np.float64) for t in (w, g, v))
+    v = f(mu) * v + g
+    o = ns_ref(g + f(mu) * v if nesterov else v, steps)
+    return w - f(lr) * (f(scale) * o + f(wd) * w), v, o
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(1, 1, 3), (1, 50, 500), (2, 75, 31), (1, 300, 140),
+                                             (2, 130, 333)])
+@pytest.mark.parametrize("nesterov,wd", [(True, 0.01), (False, 0.0)])
+def test_muon_update(batch, rows, cols, nesterov, wd):
+    print(f"muon {batch}x{rows}x{cols}", flush=True)
+    rng = np.random.default_rng([8, batch, rows, cols])
+    g, v = gradient(rng, batch, rows, cols), 3 * gradient(rng, batch, rows, cols)
+    w = (rng.standard_normal(g.shape) * 0.05).astype(np.float32)
+    wt, gt, vt = dev(w), dev(g), dev(v)
+    cc.muon_update(wt, gt, vt, 0.02, 0.95, wd, nesterov)
+    scale = max(1.0, rows / cols) ** 0.5
+    w_ref, v_ref, o = muon_ref(w, g, v, 0.02, 0.95, wd, nesterov, scale)
+    # v: a product and a sum, two roundings of 2^-24 of |mu v| + |g|
+    assert (np.abs(vt.cpu().numpy() - v_ref) <= 2.0 ** -23 * (0.95 * np.abs(v) + np.abs(g))).all()
+    # w: the step's error, and three roundings of 2^-24 of |w| + the step
+    err = np.linalg.norm(wt.double().cpu().numpy() - w_ref)
+    step = 0.02 * scale * np.linalg.norm(o)
+    assert err <= TOL * step + 2.0 ** -22 * (np.linalg.norm(w) + step)
+    assert np.array_equal(gt.cpu().numpy(), g)
+
+
+def test_muon_update_of_a_grouped_convolution():
+    """A (K, C/group, kh, kw) blob: each group's filters are one matrix."""
+    rng = np.random.default_rng(9)
+    shape = (24, 6, 3, 3)
+    g = gradient(rng, 2, 12, 54).reshape(shape)
+    w = rng.standard_normal(shape).astype(np.float32)
+    wt, vt = dev(w), torch.zeros(shape, device=DEV)
+    cc.muon_update(wt, dev(g), vt, 0.1, 0.9, scale=0.5, group=2)
+    w_ref, _, _ = muon_ref(w.reshape(2, 12, 54), g.reshape(2, 12, 54), np.zeros((2, 12, 54)), 0.1,
+                           0.9, 0.0, True, 0.5)
+    assert rel(wt, w_ref.reshape(shape)) <= TOL
+
+
+@pytest.mark.parametrize("rows,cols", [(50, 500), (260, 150)])
+def test_muon_update_captured(rows, cols):
+    """A captured update follows the rate in device memory, replay after
+    replay, with eager work between, bit for bit the eager update."""
+    rng = np.random.default_rng(10)
+    g, w = gradient(rng, 1, rows, cols), rng.standard_normal((1, rows, cols)).astype(np.float32)
+    we, ve, wg, vg = dev(w), torch.zeros(w.shape, device=DEV), dev(w), torch.zeros(w.shape,
+                                                                                    device=DEV)
+    gt, lr = dev(g), torch.empty(1, device=DEV)
+    ws = cc.Workspace()
+    ws.get(cc.newton_schulz_workspace_size(cc.ns_desc(w.shape)))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cc.muon_update(wg, gt, vg, lr, weight_decay=0.01, ws=ws)
+    for it in range(4):
+        rate = 0.1 / (it + 1)
+        cc.muon_update(we, gt, ve, rate, weight_decay=0.01)
+        lr.fill_(rate)
+        graph.replay()
+        torch.cuda.synchronize()
+        _ = torch.randn(1000, device=DEV).sum().item()
+        assert torch.equal(we, wg) and torch.equal(ve, vg), it
+
+
+def test_muon_update_refuses():
+    x = torch.zeros(4, 8, device=DEV)
+    with pytest.raises(ValueError, match="contiguous"):
+        cc.newton_schulz(torch.zeros(8, 4, device=DEV).t())
+    with pytest.raises(ValueError, match="same shape"):
+        cc.muon_update(x, x.clone(), torch.zeros(8, 4, device=DEV), 0.1)
+    with pytest.raises(ValueError, match="one element"):
+        cc.muon_update(x, x.clone(), x.clone(), torch.zeros(2, device=DEV))
+    with pytest.raises(ValueError, match="float32"):
+        cc.muon_update(x, x.bfloat16(), x.clone(), 0.1)
+    with pytest.raises(cc.CaffeError, match="ALIGN"):
+        cc.newton_schulz(torch.zeros(33, device=DEV)[1:].view(4, 8))
