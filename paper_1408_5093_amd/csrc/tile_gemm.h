@@ -158,6 +158,7 @@ struct TileNT {
             fb[j] = (rb0 >> 3) * 64 + (rb0 & 7) * 8 + (c ^ line_swz(rb0));
         }
         constexpr int FSTR = 4 * 64;  // next 32-row block
+        acc_t low[MI][NI];  // the products with a low term
 
         auto compute = [&](const u32x4* As, const u32x4* Bs, auto&& after) {
             u32x4 xa[2][Op::kFrags][MI], xb[2][Op::kFrags][NI];
@@ -184,9 +185,10 @@ struct TileNT {
 #pragma unroll
                     for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-                        for (int ni = 0; ni < NI; ++ni)
-                            acc[mi][ni] =
-                                Op::mma(xa[b][Op::fa(i)][mi], xb[b][Op::fb(i)][ni], acc[mi][ni]);
+                        for (int ni = 0; ni < NI; ++ni) {
+                            acc_t& to = i ? low[mi][ni] : acc[mi][ni];
+                            to = Op::mma(xa[b][Op::fa(i)][mi], xb[b][Op::fb(i)][ni], to);
+                        }
                 __builtin_amdgcn_sched_barrier(0);
                 after(step);
                 __builtin_amdgcn_sched_barrier(0);
@@ -197,7 +199,7 @@ struct TileNT {
         for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
             for (int ni = 0; ni < NI; ++ni)
-                acc[mi][ni] = acc_t{};
+                acc[mi][ni] = low[mi][ni] = acc_t{};
 
         issue(0, A0, B0);
         if (NS > 2 && nst > 1)
@@ -224,6 +226,13 @@ struct TileNT {
                         issue_part(t + NS - 1, An, Bn, part);
                 });
             }
+        }
+        if constexpr (Op::kProds > 1) {
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                for (int ni = 0; ni < NI; ++ni)
+                    acc[mi][ni] += low[mi][ni];
         }
     }
 
