@@ -169,11 +169,12 @@ __device__ __forceinline__ float ip8_finish(int acc, float s, float t, float bia
     return z > 0.f ? z : (relu ? 0.f : z);
 }
 
-template <int MI, int NI, int NS>
-__global__ void __launch_bounds__(256, (TileNT<OpInt8, MI, NI, NS>::kPerCu))
+typedef TileNT<OpInt8, 2, 2, 1, 1, 3, false> Ip8Tile64;
+
+template <class Tile>
+__global__ void __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd)
 ip8_tile_kernel(const Ip8Params p)
 {
-    typedef TileNT<OpInt8, MI, NI, NS> Tile;
     const int mt = (p.N + Tile::TM - 1) / Tile::TM;
     const int nt = (p.K + Tile::TN - 1) / Tile::TN;
     // consecutive tiles on one XCD, in bands of four tile rows
@@ -183,7 +184,7 @@ ip8_tile_kernel(const Ip8Params p)
         return;
     const int band = t / (4 * nt), h = min(4, mt - 4 * band), r = t - band * 4 * nt;
     const int m0 = (4 * band + r % h) * Tile::TM, n0 = r / h * Tile::TN;
-    intx16 acc[MI][NI];
+    typename Tile::acc_t acc[Tile::kMI][Tile::kNI];
     Tile::run(p.x + (size_t)m0 * p.pitch, (uint32_t)min(Tile::TM, p.N - m0) * p.pitch, p.pitch,
               p.w + (size_t)n0 * p.pitch, (uint32_t)min(Tile::TN, p.K - n0) * p.pitch, p.pitch, 0,
               (int)(p.pitch / 128), acc);
@@ -206,13 +207,13 @@ ip8_tile_kernel(const Ip8Params p)
     });
 }
 
-template <int MI, int NI, int NS>
+template <class Tile>
 hipError_t launch_ip8_tile(const Ip8Params& p, hipStream_t s)
 {
-    const int64_t tiles = (int64_t)((p.N + 64 * MI - 1) / (64 * MI)) *
-                          ((p.K + 64 * NI - 1) / (64 * NI));
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ip8_tile_kernel<MI, NI, NS>),
-                       dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), 0, s, p);
+    const int64_t tiles = (int64_t)((p.N + Tile::TM - 1) / Tile::TM) *
+                          ((p.K + Tile::TN - 1) / Tile::TN);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ip8_tile_kernel<Tile>),
+                       dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(Tile::kThreads), 0, s, p);
     return hipGetLastError();
 }
 
@@ -264,7 +265,7 @@ hipError_t launch_inner_product_int8(const Ip8Args& a, char* ws, hipStream_t s)
         p.x = q;
         p.xs = qs;
     }
-    return launch_ip8_tile<1, 1, 3>(p, s);
+    return launch_ip8_tile<Ip8Tile64>(p, s);
 }
 
 }  // namespace caffe_hip

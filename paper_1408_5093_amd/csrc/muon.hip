@@ -267,6 +267,7 @@ struct NsGemm {
     uint32_t a_pitch, b_pitch, d_pitch, d2_pitch, r_pitch;
     int M, N, stages, splits, jobs, batch;
     float mul;     // accumulator -> the value on D's scale (kEpiQ, kEpiOut: the value itself)
+    float mul2;    // ... of the second product
     float a, b, c; // kEpiQ: b on R's scale
     float d_scale; // kEpiQ: value -> D's scale
     // kEpiOut
@@ -319,13 +320,20 @@ __device__ __forceinline__ void tile_at(int t, int mt, int nt, int& I, int& J)
     }
 }
 
-template <int MI, int NI, int NS, int EPI>
-__global__ void __launch_bounds__(256, (TileNT<OpPair, MI, NI, NS>::kPerCu))
+// 64 x 64 and 128 x 128 by four waves, with accumulators for the low terms;
+// 192 x 192 by four waves and 256 x 192 by eight, whose accumulators fill the
+// registers.
+typedef TileNT<OpPairLine, 2, 2, 1, 1, 5, true> Tile64;
+typedef TileNT<OpPair, 2, 2, 2, 2, 2, true> Tile128;
+typedef TileNT<OpPair, 2, 2, 3, 3, 3, false> Tile192;
+typedef TileNT<OpPair, 4, 2, 2, 3, 2, false> Tile256;
+
+template <class Tile, int EPI>
+__global__ void __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd)
 ns_gemm_kernel(const NsGemm p)
 {
-    typedef TileNT<OpPair, MI, NI, NS> Tile;
     constexpr bool SYM = EPI == kEpiSym || EPI == kEpiQ || EPI == kEpiPart;
-    static_assert(!SYM || MI == NI, "mirrored tiles are square");
+    static_assert(!SYM || Tile::TM == Tile::TN, "mirrored tiles are square");
     const int mt = (p.M + Tile::TM - 1) / Tile::TM;
     const int nt = (p.N + Tile::TN - 1) / Tile::TN;
     const int per = SYM ? mt * (mt + 1) / 2 : mt * nt;
@@ -345,7 +353,7 @@ ns_gemm_kernel(const NsGemm p)
     const char* B = p.B[job] + b * p.b_batch + (size_t)n0 * p.b_pitch;
     const int s0 = (int)((int64_t)p.stages * split / p.splits);
     const int s1 = (int)((int64_t)p.stages * (split + 1) / p.splits);
-    floatx16 acc[MI][NI];
+    typename Tile::acc_t acc[Tile::kMI][Tile::kNI];
     Tile::run(A, (uint32_t)min(Tile::TM, p.M - m0) * p.a_pitch, p.a_pitch, B,
               (uint32_t)min(Tile::TN, p.N - n0) * p.b_pitch, p.b_pitch, s0, s1 - s0, acc);
 
@@ -354,6 +362,7 @@ ns_gemm_kernel(const NsGemm p)
         char* D = p.D[job] + b * p.d_batch;
         const int kp = (int)(p.d_pitch / 4);
         const bool mirror = I != J;
+        const float mul = job ? p.mul2 : p.mul;
         Tile::each(acc, [&](int di, int dj, float(&v)[4]) {
             const int i = m0 + di, j = n0 + dj;
             if constexpr (EPI == kEpiQ) {
@@ -367,7 +376,7 @@ ns_gemm_kernel(const NsGemm p)
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    v[e] *= p.mul;
+                    v[e] *= mul;
             }
             if (mirror && j < p.M && i < kp)
                 store_pair4(D, pair_off(p.d_pitch, j, i), v);
@@ -448,22 +457,53 @@ ns_reduce_kernel(const float* __restrict__ part, int splits, int m, char* __rest
 }
 
 // --------------------------------------------------------------------- host
-template <int MI, int NI, int NS, int EPI>
-hipError_t launch_tile(const NsGemm& p, hipStream_t s)
+template <class Tile, int EPI>
+int64_t tile_count(const NsGemm& p)
 {
     constexpr bool SYM = EPI == kEpiSym || EPI == kEpiQ || EPI == kEpiPart;
-    const int64_t mt = (p.M + 64 * MI - 1) / (64 * MI), nt = (p.N + 64 * NI - 1) / (64 * NI);
-    const int64_t tiles =
-        (SYM ? mt * (mt + 1) / 2 : mt * nt) * p.jobs * p.splits * p.batch;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ns_gemm_kernel<MI, NI, NS, EPI>),
-                       dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), 0, s, p);
+    const int64_t mt = (p.M + Tile::TM - 1) / Tile::TM, nt = (p.N + Tile::TN - 1) / Tile::TN;
+    return (SYM ? mt * (mt + 1) / 2 : mt * nt) * p.jobs * p.splits * p.batch;
+}
+
+template <class Tile, int EPI>
+hipError_t launch_tile(const NsGemm& p, hipStream_t s)
+{
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ns_gemm_kernel<Tile, EPI>),
+                       dim3((unsigned)((tile_count<Tile, EPI>(p) + 7) / 8 * 8)),
+                       dim3(Tile::kThreads), 0, s, p);
     return hipGetLastError();
 }
 
+// The tile by a model of the time on 256 compute units: `over` us for a launch
+// and its epilogue, and per stage of 32 reduction elements `one` us while every
+// unit has at most one tile, else `each` us for each tile of the fullest unit.
+// Fitted to 200 x 200 .. 4096 x 9216; us measured / modelled, symmetric
+// products m = 512 .. 4096 and 4096 x 9216 x 4096:
+//          512       1280      1800      2560      3000       4096       x 9216
+//   64     8 / 8     15 / 15   33 / 34   93 / 90   129 / 130  255 / 315  1090 / 1250
+//   128    20 / 20   40 / 42   51 / 57   80 / 78   126 / 130  240 / 260  790 / 766
+//   192    33 / 33   56 / 64   73 / 86   101 / 116 125 / 134  185 / 178  900 / 844
+//   256 x 192 (full products only)                                       755 / 745
 template <int EPI>
 hipError_t launch_gemm(const NsGemm& p, hipStream_t s)
 {
-    return launch_tile<1, 1, 3, EPI>(p, s);
+    auto cost = [&](int64_t tiles, double over, double one, double each) {
+        const int64_t n = (tiles + 255) / 256;
+        return over + p.stages * (n <= 1 ? one : each * (double)n);
+    };
+    const double c64 = cost(tile_count<Tile64, EPI>(p), 3.5, 0.29, 0.27);
+    const double c128 = cost(tile_count<Tile128, EPI>(p), 6.0, 0.90, 0.66);
+    const double c192 = cost(tile_count<Tile192, EPI>(p), 12.0, 1.30, 1.30);
+    if constexpr (EPI == kEpiX || EPI == kEpiOut) {
+        const double c256 = cost(tile_count<Tile256, EPI>(p), 15.0, 1.90, 1.90);
+        if (c256 < c64 && c256 < c128 && c256 < c192)
+            return launch_tile<Tile256, EPI>(p, s);
+    }
+    if (c192 < c64 && c192 < c128)
+        return launch_tile<Tile192, EPI>(p, s);
+    if (c128 < c64)
+        return launch_tile<Tile128, EPI>(p, s);
+    return launch_tile<Tile64, EPI>(p, s);
 }
 
 int exponent_for(double bound)  // bound * 2^result <= 2^14
@@ -655,7 +695,7 @@ hipError_t launch_newton_schulz(const NsPlan& q, const NsArgs& x, char* ws, hipS
             p.mul = ldexpf(1.f, er - 2 * ex);
             if (q.splits > 1) {
                 p.part = (float*)(ws + q.off_split);
-                e = launch_tile<1, 1, 3, kEpiPart>(p, s);
+                e = launch_tile<Tile64, kEpiPart>(p, s);
                 if (e != hipSuccess)
                     return e;
                 hipLaunchKernelGGL(ns_reduce_kernel,
@@ -692,18 +732,20 @@ hipError_t launch_newton_schulz(const NsPlan& q, const NsArgs& x, char* ws, hipS
             const int et = exponent_for(q.qmax[k] * q.bound[k]);
             const int ep2 = exponent_for(pbound);
             char* P2 = spare;
-            if (more) {
-                p = square(Q, R, T);
-                p.mul = ldexpf(1.f, et - eq - er);
-                if ((e = launch_gemm<kEpiSym>(p, s)) != hipSuccess)
-                    return e;
-            }
+            // T = Q R and P = Q P, neither of which waits for the other
+            p = square(Q, R, T);
+            p.mul = ldexpf(1.f, et - eq - er);
             if (P) {
-                p = square(Q, P, P2);
-                p.mul = ldexpf(1.f, ep2 - eq - ep);
+                const int j = more ? 1 : 0;
+                p.A[j] = Q;
+                p.B[j] = P;
+                p.D[j] = P2;
+                (j ? p.mul2 : p.mul) = ldexpf(1.f, ep2 - eq - ep);
+                p.jobs = j + 1;
+            }
+            if (more || P)
                 if ((e = launch_gemm<kEpiSym>(p, s)) != hipSuccess)
                     return e;
-            }
             if (more) {
                 er = exponent_for(q.bound[k + 1]);
                 p = square(T, Q, R);

@@ -1,6 +1,6 @@
 // tile_gemm.h -- the tile product that the dense operators share (the matrix
-// products of muon.hip, the 8-bit inner product of int8.hip): a workgroup of
-// four waves forms a TM x TN tile of A B^T from operands whose rows are runs
+// products of muon.hip, the 8-bit inner product of int8.hip): a workgroup
+// forms a TM x TN tile of A B^T from operands whose rows are runs
 // of 128-byte lines along the reduction index.
 //
 // One stage is one line of every operand row.  A line holds eight 16-byte
@@ -11,8 +11,8 @@
 //
 // Lines go global -> LDS by 16-byte DMA, eight rows per wave copy, chunk c of
 // tile row r at slot c ^ line_swz(r): fragment reads of consecutive rows then
-// spread over the banks.  NS buffers: the copies of stage t + NS - 1 go out
-// among the instructions of stage t.
+// spread over the banks.  NS buffers; the instructions of a step carry the
+// fragment reads of the next step and a share of the copies between them.
 #pragma once
 
 #include "device_common.h"
@@ -33,11 +33,22 @@ struct OpPair {
     static constexpr int frag(int step, int f) { return step + 2 * f; }
     static constexpr int fa(int i) { return i == 2 ? 1 : 0; }
     static constexpr int fb(int i) { return i == 1 ? 1 : 0; }
+    static constexpr bool low(int i) { return i % 3 != 0; }  // with a low term
     static __device__ __forceinline__ acc_t mma(u32x4 a, u32x4 b, acc_t c)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a),
                                                       __builtin_bit_cast(halfx8, b), c, 0, 0, 0);
     }
+};
+
+// The same with the whole line as one step: a small tile, with few
+// instructions to a step, then has a whole stage's time for its fragment
+// reads.
+struct OpPairLine : OpPair {
+    static constexpr int kSteps = 1, kFrags = 4, kProds = 6;
+    static constexpr int frag(int, int f) { return f; }
+    static constexpr int fa(int i) { return i % 3 == 2 ? i / 3 + 2 : i / 3; }
+    static constexpr int fb(int i) { return i % 3 == 1 ? i / 3 + 2 : i / 3; }
 };
 
 // 8-bit integers: a line is 128 reduction elements.
@@ -47,6 +58,7 @@ struct OpInt8 {
     static constexpr int frag(int step, int) { return step; }
     static constexpr int fa(int) { return 0; }
     static constexpr int fb(int) { return 0; }
+    static constexpr bool low(int) { return false; }
     static __device__ __forceinline__ acc_t mma(u32x4 a, u32x4 b, acc_t c)
     {
         return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(intx4, a),
@@ -84,13 +96,27 @@ __device__ __forceinline__ void tile_wait()  // s_waitcnt vmcnt(N)
     __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (((N >> 4) & 3) << 14));
 }
 
-template <class Op, int MI, int NI, int NS>
+// s_waitcnt vmcnt(N) lgkmcnt(0): also this wave's LDS reads
+template <int N>
+__device__ __forceinline__ void tile_wait_lds()
+{
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (((N >> 4) & 3) << 14));
+}
+
+// WM x WN waves of 32 MI x 32 NI each; LOW: products with a low term have
+// accumulators of their own (kProds > 1), so that they do not round the sum.
+template <class Op, int WM, int WN, int MI, int NI, int NS, bool LOW>
 struct TileNT {
-    static constexpr int TM = 64 * MI, TN = 64 * NI;  // 2 x 2 waves of 32 MI x 32 NI
+    static constexpr int NW = WM * WN;
+    static constexpr int TM = 32 * WM * MI, TN = 32 * WN * NI;
+    static constexpr int kThreads = 64 * NW;
+    static constexpr int kMI = MI, kNI = NI;
     static constexpr int kLdsBytes = (TM + TN) * 128 * NS;
-    // workgroups that one compute unit's LDS holds, at most the four of a full
-    // register file's halves
+    // workgroups that one compute unit's LDS holds, and with them the waves on
+    // each of its four SIMDs: the register budget
     static constexpr int kPerCu = 160 * 1024 / kLdsBytes > 4 ? 4 : 160 * 1024 / kLdsBytes;
+    static constexpr int kWavesPerSimd = kPerCu * NW / 4;
     typedef typename Op::acc_t acc_t;
 
     // acc = A B^T over stages s0 .. s0 + nst - 1 (nst >= 1).  A points at the
@@ -100,29 +126,33 @@ struct TileNT {
                                                const void* B, uint32_t b_bytes, uint32_t b_pitch,
                                                int s0, int nst, acc_t (&acc)[MI][NI])
     {
-        constexpr int NA = 2 * MI, NB = 2 * NI;  // copies per wave and stage
-        __shared__ u32x4 A0[TM * 8], A1[TM * 8], A2[NS > 2 ? TM * 8 : 1];
-        __shared__ u32x4 B0[TN * 8], B1[TN * 8], B2[NS > 2 ? TN * 8 : 1];
-        static_assert(NS == 2 || NS == 3, "buffers");
+        constexpr int NA = TM / 8 / NW, NB = TN / 8 / NW;  // copies per wave and stage
+        static_assert(TM % (8 * NW) == 0 && TN % (8 * NW) == 0 && NW % 2 == 0, "copy mapping");
+        // one array per buffer, A's rows then B's: the compiler tells the copies
+        // to one from the reads of another by the array (it follows eight)
+        static_assert(NS >= 2 && NS <= 8, "buffers");
+        constexpr int kBuf = (TM + TN) * 8;
+        __shared__ u32x4 L0[kBuf], L1[kBuf], L2[NS > 2 ? kBuf : 1], L3[NS > 3 ? kBuf : 1];
+        __shared__ u32x4 L4[NS > 4 ? kBuf : 1], L5[NS > 5 ? kBuf : 1], L6[NS > 6 ? kBuf : 1];
+        __shared__ u32x4 L7[NS > 7 ? kBuf : 1];
+        u32x4* const Lb[8] = {L0, L1, L2, L3, L4, L5, L6, L7};
 
         const int tid = threadIdx.x;
         const int lane = tid & 63;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const int wm = wave & 1, wn = wave >> 1;
-        const __amdgpu_buffer_rsrc_t ra = make_rsrc(A, a_bytes);
-        const __amdgpu_buffer_rsrc_t rb = make_rsrc(B, b_bytes);
+        const int wm = wave % WM, wn = wave / WM;
 
-        // copy i = wave + 4 q moves tile rows 8 i .. 8 i + 7; of i, line_swz
+        // copy i = wave + NW q moves tile rows 8 i .. 8 i + 7; of i, line_swz
         // sees only bit 3 of the row, the wave's parity
         const int cr = lane >> 3;
         const uint32_t ck = 16u * ((lane & 7) ^ line_swz(8 * wave + cr));
         uint32_t va[NA], vb[NB];
 #pragma unroll
         for (int q = 0; q < NA; ++q)
-            va[q] = (uint32_t)(8 * (wave + 4 * q) + cr) * a_pitch + ck;
+            va[q] = (uint32_t)(8 * (wave + NW * q) + cr) * a_pitch + ck;
 #pragma unroll
         for (int q = 0; q < NB; ++q)
-            vb[q] = (uint32_t)(8 * (wave + 4 * q) + cr) * b_pitch + ck;
+            vb[q] = (uint32_t)(8 * (wave + NW * q) + cr) * b_pitch + ck;
 #pragma unroll
         for (int q = 0; q < NA; ++q)
             va[q] = va[q] < a_bytes ? va[q] : kOob;
@@ -130,22 +160,18 @@ struct TileNT {
         for (int q = 0; q < NB; ++q)
             vb[q] = vb[q] < b_bytes ? vb[q] : kOob;
 
+        // copy c of the wave's NC of stage t; past the last stage it lands zeros
+        // and reads nothing, so that the number of copies in flight is known
+        // everywhere (a copy in a branch made the compiler wait for all of them)
         constexpr int NC = NA + NB;
-        constexpr int CPP = (NC + Op::kSteps - 1) / Op::kSteps;
-        auto issue_part = [&](int t, u32x4* As, u32x4* Bs, int part) {
+        auto copy = [&](int t, u32x4* L, int c) {
             const uint32_t soff = (uint32_t)(s0 + t) * 128u;
-#pragma unroll
-            for (int c = part * CPP; c < (part + 1) * CPP && c < NC; ++c) {
-                if (c < NA)
-                    line_copy(ra, &As[(wave + 4 * c) * 64], va[c], soff);
-                else
-                    line_copy(rb, &Bs[(wave + 4 * (c - NA)) * 64], vb[c - NA], soff);
-            }
-        };
-        auto issue = [&](int t, u32x4* As, u32x4* Bs) {
-#pragma unroll
-            for (int part = 0; part < Op::kSteps; ++part)
-                issue_part(t, As, Bs, part);
+            if (c < NA)
+                line_copy(make_rsrc(A, t < nst ? a_bytes : 0u), &L[(wave + NW * c) * 64], va[c],
+                          soff);
+            else
+                line_copy(make_rsrc(B, t < nst ? b_bytes : 0u),
+                          &L[TM * 8 + (wave + NW * (c - NA)) * 64], vb[c - NA], soff);
         };
 
         const int ra0 = wm * MI * 32 + (lane & 31);
@@ -155,42 +181,42 @@ struct TileNT {
         for (int j = 0; j < 4; ++j) {
             const int c = 2 * j + (lane >> 5);
             fa[j] = (ra0 >> 3) * 64 + (ra0 & 7) * 8 + (c ^ line_swz(ra0));
-            fb[j] = (rb0 >> 3) * 64 + (rb0 & 7) * 8 + (c ^ line_swz(rb0));
+            fb[j] = TM * 8 + (rb0 >> 3) * 64 + (rb0 & 7) * 8 + (c ^ line_swz(rb0));
         }
         constexpr int FSTR = 4 * 64;  // next 32-row block
-        acc_t low[MI][NI];  // the products with a low term
+        acc_t low[LOW ? MI : 1][LOW ? NI : 1];
 
-        auto compute = [&](const u32x4* As, const u32x4* Bs, auto&& after) {
-            u32x4 xa[2][Op::kFrags][MI], xb[2][Op::kFrags][NI];
-            auto read = [&](int step, int b) {
+        constexpr int S = Op::kSteps;
+        constexpr int NR = Op::kFrags * (MI + NI);  // fragment reads of a step
+        constexpr int NM = Op::kProds * MI * NI;    // instructions of a step
+        // copies of a step: all at once where two buffers leave one stage's time
+        constexpr int CPS = NS == 2 ? NC : (NC + S - 1) / S;
+        u32x4 xa[2][Op::kFrags][MI], xb[2][Op::kFrags][NI];
+        auto read = [&](const u32x4* L, int step, int r, int b) {
+            const int f = r / (MI + NI), k = r % (MI + NI);
+            if (k < MI)
+                xa[b][f][k] = L[fa[Op::frag(step, f)] + k * FSTR];
+            else
+                xb[b][f][k - MI] = L[fb[Op::frag(step, f)] + (k - MI) * FSTR];
+        };
+        // The instructions of a step, with the next step's fragment reads
+        // (from Lr) and a share of a stage's copies (part `part` of stage ct to
+        // Lc) spread among them.
+        auto run_step = [&](int b, int next, const u32x4* Lr, int ct, u32x4* Lc, int part) {
 #pragma unroll
-                for (int f = 0; f < Op::kFrags; ++f) {
+            for (int m = 0; m < NM; ++m) {
 #pragma unroll
-                    for (int mi = 0; mi < MI; ++mi)
-                        xa[b][f][mi] = As[fa[Op::frag(step, f)] + mi * FSTR];
+                for (int r = 0; r < NR; ++r)
+                    if (r * (NM - NM / 4) / NR == m)
+                        read(Lr, next, r, b ^ 1);
 #pragma unroll
-                    for (int ni = 0; ni < NI; ++ni)
-                        xb[b][f][ni] = Bs[fb[Op::frag(step, f)] + ni * FSTR];
-                }
-            };
-            read(0, 0);
-#pragma unroll
-            for (int step = 0; step < Op::kSteps; ++step) {
-                const int b = step & 1;
-                if (step + 1 < Op::kSteps)
-                    read(step + 1, b ^ 1);
+                for (int c = 0; c < CPS; ++c)
+                    if (c * NM / CPS == m && part * CPS + c < NC)
+                        copy(ct, Lc, part * CPS + c);
                 __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int i = 0; i < Op::kProds; ++i)
-#pragma unroll
-                    for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-                        for (int ni = 0; ni < NI; ++ni) {
-                            acc_t& to = i ? low[mi][ni] : acc[mi][ni];
-                            to = Op::mma(xa[b][Op::fa(i)][mi], xb[b][Op::fb(i)][ni], to);
-                        }
-                __builtin_amdgcn_sched_barrier(0);
-                after(step);
+                const int i = m / (MI * NI), mi = m / NI % MI, ni = m % NI;
+                acc_t& to = LOW && Op::low(i) ? low[LOW ? mi : 0][LOW ? ni : 0] : acc[mi][ni];
+                to = Op::mma(xa[b][Op::fa(i)][mi], xb[b][Op::fb(i)][ni], to);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -199,35 +225,51 @@ struct TileNT {
         for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
             for (int ni = 0; ni < NI; ++ni)
-                acc[mi][ni] = low[mi][ni] = acc_t{};
-
-        issue(0, A0, B0);
-        if (NS > 2 && nst > 1)
-            issue(1, A1, B1);
-        for (int t0 = 0; t0 < nst; t0 += NS) {
+                acc[mi][ni] = acc_t{};
+        if constexpr (LOW) {
 #pragma unroll
-            for (int h = 0; h < NS; ++h) {
-                const int t = t0 + h;
+            for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                for (int ni = 0; ni < NI; ++ni)
+                    low[mi][ni] = acc_t{};
+        }
+
+        // Stage t + NS goes to stage t's buffer once every wave has read its
+        // last fragments from it, before the last step of stage t: copies in
+        // that step and (with more than two buffers) in the next stage's others.
+        constexpr int P = NS - 1;  // (h + P) % NS: the buffer before h
+#pragma unroll
+        for (int t = 0; t < NS; ++t)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (t < P || CPS == NC || c < CPS)
+                    copy(t, Lb[t], c);
+        tile_wait<(NS - 2) * NC + CPS>();
+        tile_barrier();
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+            read(L0, 0, r, 0);
+        // whole turns of the buffers and of the two sets of fragments
+        constexpr int U = NS * S % 2 ? 2 * NS : NS;
+        for (int t0 = 0; t0 < nst; t0 += U) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int t = t0 + u, h = u % NS;
                 if (t >= nst)
                     break;
-                u32x4* Ac = h == 0 ? A0 : (h == 1 ? A1 : A2);
-                u32x4* Bc = h == 0 ? B0 : (h == 1 ? B1 : B2);
-                const int hn = (h + NS - 1) % NS;
-                u32x4* An = hn == 0 ? A0 : (hn == 1 ? A1 : A2);
-                u32x4* Bn = hn == 0 ? B0 : (hn == 1 ? B1 : B2);
-                if (NS > 2 && t + 1 < nst)
-                    tile_wait<NA + NB>();
-                else
-                    tile_wait<0>();
+                // the rest of stage t - 1 + NS
+#pragma unroll
+                for (int step = 0; step + 1 < S; ++step)
+                    run_step((u * S + step) & 1, step + 1, Lb[h], t + P, Lb[(h + P) % NS],
+                             step + 1);
+                // stage t + 1 is there, stages t + 2 .. t + NS - 1 may be in flight
+                tile_wait_lds<(NS - 2) * NC>();
                 tile_barrier();
-                const bool more = t + NS - 1 < nst;
-                compute(Ac, Bc, [&](int part) {
-                    if (more)
-                        issue_part(t + NS - 1, An, Bn, part);
-                });
+                run_step((u * S + S - 1) & 1, 0, Lb[(h + 1) % NS], t + NS, Lb[h], 0);
             }
         }
-        if constexpr (Op::kProds > 1) {
+        tile_wait<0>();  // no copy outlives the workgroup's LDS
+        if constexpr (LOW) {
 #pragma unroll
             for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
@@ -243,7 +285,7 @@ struct TileNT {
     {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int wm = wave & 1, wn = wave >> 1;
+        const int wm = wave % WM, wn = wave / WM;
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
