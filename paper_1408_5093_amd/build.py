@@ -39,6 +39,7 @@ EXTRA = {
     "conv_triple.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "conv_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "muon.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "muon_small.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "int8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 

@@ -555,11 +555,19 @@ struct NsPlan {
     int batch, rows, cols, m, n, tall, steps, segments, splits, norm_blocks;
     double bound[kNsMaxSteps + 1];  // of the squared singular values before step k
     double qmax[kNsMaxSteps];       // of |q| over them
+    double pmax[kNsMaxSteps];       // of the segment's product of q up to step k
     int length[kNsMaxSteps];        // steps of each segment
     size_t m_pitch, n_pitch;        // bytes of a row of m (n) elements in two terms
     size_t mm_bytes, xr_bytes, xt_bytes;
     size_t off_part, off_split, off_xr, off_xt[2], off_mm[5], ws_bytes;
+    // a side of at most 128 (muon_small.hip): column chunks, their slabs, the
+    // parts of the Gram matrix; everything in one launch (solo)
+    int small, solo, chunks, slabs, parts;
+    size_t part_bytes, img_bytes, xs_bytes;  // of one matrix
 };
+constexpr int kNsSmall = 128;
+constexpr int kNsSoloChunks = 4;
+int ns_exponent(double bound);  // bound * 2^result <= 2^14
 // false: the coefficients let the iteration leave kNsMaxRange.
 bool ns_plan(int batch, int rows, int cols, int steps, float a, float b, float c, NsPlan* plan);
 struct NsArgs {

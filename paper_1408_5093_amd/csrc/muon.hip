@@ -30,129 +30,17 @@
 // no element can leave the half type's range, whatever the matrix.  Three
 // products (high high, high low, low high) give the accuracy of a float
 // product: the missing low low term is 2^-22 of it.
-#include <math.h>
-
 #include <algorithm>
 #include <type_traits>
 
-#include "tile_gemm.h"
+#include "ns_device.h"
 
 namespace caffe_hip {
 
 namespace {
 
-typedef _Float16 halfx4 __attribute__((ext_vector_type(4)));
-typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
-
-// ------------------------------------------------------------ pair matrices
-// Element (row, k): line k / 32 of the row, its high half at byte 2 (k % 32),
-// its low half 64 bytes on.  k a multiple of 4.
-__device__ __forceinline__ size_t pair_off(size_t pitch, int row, int k)
-{
-    return (size_t)row * pitch + (size_t)(k >> 5) * 128 + (k & 31) * 2;
-}
-
-__device__ __forceinline__ void store_pair4(char* M, size_t off, const float (&v)[4])
-{
-    halfx4 h, l;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        h[e] = (_Float16)v[e];
-        l[e] = (_Float16)(v[e] - (float)h[e]);
-    }
-    *(halfx4*)(M + off) = h;
-    *(halfx4*)(M + off + 64) = l;
-}
-
-__device__ __forceinline__ void load_pair4(const char* M, size_t off, float (&v)[4])
-{
-    const halfx4 h = *(const halfx4*)(M + off), l = *(const halfx4*)(M + off + 64);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        v[e] = (float)h[e] + (float)l[e];
-}
-
 // --------------------------------------------------------------- first pass
-// u (the matrix to orthogonalise) is g, or with momentum
-// v <- mu v + g (written) and u = nesterov ? g + mu v : v.
-struct NsInput {
-    const void* g;
-    float* v;       // null: u = g
-    float mu;
-    int nesterov;
-    int bf16;       // g is bfloat16 (v null)
-    int64_t count;  // elements of one matrix
-};
-
-template <int VEC>
-__device__ __forceinline__ void load_vec(const NsInput& in, int64_t at, float (&g)[VEC])
-{
-    if (in.bf16) {
-        const uint16_t* p = (const uint16_t*)in.g + at;
-        if constexpr (VEC == 4) {
-            const u16x4 x = *(const u16x4*)p;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                g[e] = bf16_to_f32(x[e]);
-        } else {
-            g[0] = bf16_to_f32(*p);
-        }
-    } else {
-        const float* p = (const float*)in.g + at;
-        if constexpr (VEC == 4) {
-            const floatx4 x = *(const floatx4*)p;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                g[e] = x[e];
-        } else {
-            g[0] = *p;
-        }
-    }
-}
-
-template <int VEC>
-__device__ __forceinline__ void load_u(const NsInput& in, int64_t at, bool update, float (&u)[VEC])
-{
-    load_vec<VEC>(in, at, u);
-    if (in.v) {
-        float* p = in.v + at;
-        float v[VEC];
-        if constexpr (VEC == 4) {
-            const floatx4 x = *(const floatx4*)p;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = x[e];
-        } else {
-            v[0] = *p;
-        }
-        if (update) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                v[e] = in.mu * v[e] + u[e];
-            if constexpr (VEC == 4)
-                *(floatx4*)p = floatx4{v[0], v[1], v[2], v[3]};
-            else
-                *p = v[0];
-        }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            u[e] = in.nesterov ? u[e] + in.mu * v[e] : v[e];
-    }
-}
-
 constexpr int kNormBlocks = 256;  // partial sums of one matrix, at most
-
-__device__ __forceinline__ double block_sum(double s)
-{
-    __shared__ double part[4];
-    for (int off = 32; off > 0; off >>= 1)
-        s += __shfl_xor(s, off, 64);
-    if ((threadIdx.x & 63) == 0)
-        part[threadIdx.x >> 6] = s;
-    __syncthreads();
-    s = (part[0] + part[1]) + (part[2] + part[3]);
-    return s;
-}
 
 // The momentum update and each block's part of ||u||^2, in double (squares of
 // floats neither overflow nor vanish there).  Bound by HBM.
@@ -170,17 +58,9 @@ ns_norm_kernel(const NsInput in, double* __restrict__ part)
         for (int e = 0; e < VEC; ++e)
             s += (double)u[e] * (double)u[e];
     }
-    s = block_sum(s);
+    s = block_sum<4>(s);
     if (threadIdx.x == 0)
         part[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
-}
-
-// 1 / (||u|| + eps), 0 for a zero matrix, NaN where an element is NaN or
-// infinite; the parts are added in a fixed order.
-__device__ __forceinline__ double inv_norm(const double* part, int parts, double eps)
-{
-    const double s = block_sum((int)threadIdx.x < parts ? part[threadIdx.x] : 0.0);
-    return s == 0.0 ? 0.0 : (s < INFINITY ? 1.0 / (sqrt(s) + eps) : NAN);
 }
 
 // u / norm as pair matrices in both orders: rows along u's columns (Nl) and
@@ -202,7 +82,7 @@ ns_stage_kernel(const NsStage p)
 {
     __shared__ float tile[64][65];
     const int b = blockIdx.z;
-    const double inv = inv_norm(p.part + (size_t)b * p.parts, p.parts, p.eps) * p.scale;
+    const double inv = inv_norm<4>(p.part + (size_t)b * p.parts, p.parts, p.eps) * p.scale;
     const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
     const int64_t base = (int64_t)b * p.in.count;
     const int nk = (int)(p.n_pitch / 4), tk = (int)(p.t_pitch / 4);  // padded reduction lengths
@@ -506,14 +386,14 @@ hipError_t launch_gemm(const NsGemm& p, hipStream_t s)
     return launch_tile<Tile64, EPI>(p, s);
 }
 
-int exponent_for(double bound)  // bound * 2^result <= 2^14
+}  // namespace
+
+int ns_exponent(double bound)
 {
     int e;
     frexp(bound, &e);
     return 14 - e;
 }
-
-}  // namespace
 
 // The ranges of t q(t)^2 and q(t) over t in [0, top]: their extremes lie at
 // the ends or where a derivative vanishes.
@@ -579,6 +459,11 @@ bool ns_plan(int batch, int rows, int cols, int steps, float a, float b, float c
         left -= q->length[i];
     }
     q->length[0] = left;
+    for (int i = 0, k = 0; i < q->segments; ++i) {
+        double pb = 1.0;
+        for (int l = 0; l < q->length[i]; ++l, ++k)
+            q->pmax[k] = pb = std::max(pb * q->qmax[k], 1e-9);
+    }
     const size_t align = 255;
     const size_t mp = (size_t)((q->m + 31) / 32) * 128, np = (size_t)((q->n + 31) / 32) * 128;
     q->m_pitch = mp;
@@ -603,6 +488,15 @@ bool ns_plan(int batch, int rows, int cols, int steps, float a, float b, float c
         return at;
     };
     q->off_part = take((size_t)batch * q->norm_blocks * sizeof(double));
+    q->small = q->m <= kNsSmall;
+    if (q->small) {
+        ns_small_sizes(q->m, q->n, q);
+        q->off_split = take(batch * q->part_bytes);
+        q->off_mm[0] = take(batch * q->img_bytes);
+        q->off_xt[0] = take(q->segments > 1 ? batch * q->xs_bytes : 0);
+        q->ws_bytes = off;
+        return true;
+    }
     q->off_split = take(q->splits > 1 ? (size_t)batch * q->splits * q->m * q->m * 4 : 0);
     q->off_xr = take(batch * q->xr_bytes);
     q->off_xt[0] = take(batch * q->xt_bytes);
@@ -625,15 +519,19 @@ hipError_t launch_newton_schulz(const NsPlan& q, const NsArgs& x, char* ws, hipS
     in.nesterov = x.nesterov;
     in.bf16 = x.bf16;
     in.count = count;
+    if (q.small && q.solo)
+        return launch_ns_small(q, in, x, ws, s);
     double* part = (double*)(ws + q.off_part);
     const dim3 ng((unsigned)q.norm_blocks, (unsigned)q.batch);
     if (count % 4 == 0)
         hipLaunchKernelGGL(ns_norm_kernel<4>, ng, dim3(256), 0, s, in, part);
     else
         hipLaunchKernelGGL(ns_norm_kernel<1>, ng, dim3(256), 0, s, in, part);
+    if (q.small)
+        return launch_ns_small(q, in, x, ws, s);
 
     char *xr = ws + q.off_xr, *xt = ws + q.off_xt[0], *xt2 = ws + q.off_xt[1];
-    int ex = exponent_for(1.0);
+    int ex = ns_exponent(1.0);
     NsStage st{};
     st.in = in;
     st.part = part;
@@ -678,7 +576,7 @@ hipError_t launch_newton_schulz(const NsPlan& q, const NsArgs& x, char* ws, hipS
     for (int seg = 0; seg < q.segments; ++seg) {
         const int L = q.length[seg];
         // R = X X^T
-        int er = exponent_for(q.bound[k]);
+        int er = ns_exponent(q.bound[k]);
         {
             NsGemm p{};
             p.A[0] = p.B[0] = xr;
@@ -712,12 +610,11 @@ hipError_t launch_newton_schulz(const NsPlan& q, const NsArgs& x, char* ws, hipS
         }
         char* P = nullptr;
         int ep = 0;
-        double pbound = 1.0;
         for (int l = 0; l < L; ++l, ++k) {
             // Q = a I + b R + c R R; the segment's first is its P as well
             char* spare = ws + q.off_mm[P == ws + q.off_mm[3] ? 4 : 3];
             char* Q = P ? Qm : spare;
-            const int eq = exponent_for(q.qmax[k]);
+            const int eq = ns_exponent(q.qmax[k]);
             NsGemm p = square(R, R, Q);
             p.R = R;
             p.mul = ldexpf(1.f, -2 * er);
@@ -727,10 +624,9 @@ hipError_t launch_newton_schulz(const NsPlan& q, const NsArgs& x, char* ws, hipS
             p.d_scale = ldexpf(1.f, eq);
             if ((e = launch_gemm<kEpiQ>(p, s)) != hipSuccess)
                 return e;
-            pbound *= q.qmax[k];
             const bool more = l + 1 < L;
-            const int et = exponent_for(q.qmax[k] * q.bound[k]);
-            const int ep2 = exponent_for(pbound);
+            const int et = ns_exponent(q.qmax[k] * q.bound[k]);
+            const int ep2 = ns_exponent(q.pmax[k]);
             char* P2 = spare;
             // T = Q R and P = Q P, neither of which waits for the other
             p = square(Q, R, T);
@@ -747,7 +643,7 @@ hipError_t launch_newton_schulz(const NsPlan& q, const NsArgs& x, char* ws, hipS
                 if ((e = launch_gemm<kEpiSym>(p, s)) != hipSuccess)
                     return e;
             if (more) {
-                er = exponent_for(q.bound[k + 1]);
+                er = ns_exponent(q.bound[k + 1]);
                 p = square(T, Q, R);
                 p.mul = ldexpf(1.f, er - et - eq);
                 if ((e = launch_gemm<kEpiSym>(p, s)) != hipSuccess)
@@ -769,7 +665,7 @@ hipError_t launch_newton_schulz(const NsPlan& q, const NsArgs& x, char* ws, hipS
         p.splits = p.jobs = 1;
         p.batch = q.batch;
         if (seg + 1 < q.segments) {
-            const int ex2 = exponent_for(sqrt(q.bound[k]));
+            const int ex2 = ns_exponent(sqrt(q.bound[k]));
             p.D[0] = xr;
             p.D2 = xt2;
             p.d_batch = q.xr_bytes;
