@@ -566,7 +566,6 @@ struct NsPlan {
     size_t part_bytes, img_bytes, xs_bytes;  // of one matrix
 };
 constexpr int kNsSmall = 128;
-constexpr int kNsSoloChunks = 4;
 int ns_exponent(double bound);  // bound * 2^result <= 2^14
 // false: the coefficients let the iteration leave kNsMaxRange.
 bool ns_plan(int batch, int rows, int cols, int steps, float a, float b, float c, NsPlan* plan);

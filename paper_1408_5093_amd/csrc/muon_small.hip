@@ -39,8 +39,9 @@ struct Small {
     static constexpr int kTiles = MT * (MT + 1) / 2;      // 32 x 32 below the diagonal
     static constexpr int kSplit = MT == 1 ? 8 : (MT == 2 ? 2 : 1);  // waves to a tile
     static constexpr int kOwn = (kTiles * kSplit + kWaves - 1) / kWaves;
-    static constexpr int kLds =
-        kImage + (kImage > LD * kChunkPitch ? kImage : LD * kChunkPitch);
+    static constexpr int kShares = kSplit > 1 ? kWaves * 16 * 64 * 4 : 0;
+    static constexpr int kChunkBytes = LD * kChunkPitch > kShares ? LD * kChunkPitch : kShares;
+    static constexpr int kLds = kImage + (kImage > kChunkBytes ? kImage : kChunkBytes);
     typedef float Panel[T16][4];
 
     static __device__ __forceinline__ void store_panel(char* img, int row, const Panel& d,
@@ -86,7 +87,7 @@ struct Small {
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 y[I][q] = (hi[q] + lo[q]) * mul;
-            if (I & 1)  // (all reads at once would not fit the registers)
+            if (MT > 2 && I & 1)  // (all reads at once would not fit the registers)
                 __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -142,7 +143,7 @@ __device__ __forceinline__ void load_columns(const NsSmall& p, int b, int j, dou
 enum { kGram = 0, kApplyGram = 1, kApplyOut = 2 };
 
 // Column chunks c0 .. c1 - 1 of X: with kApply* X <- P X, then the chunks'
-// part of X X^T (to part numbers slab * kSplit ..), or the result.  P's image is
+// part of X X^T (part number slab_no), or the result.  P's image is
 // in LDS already where p_img is null.
 template <int MT, int VEC, int MODE>
 __device__ __forceinline__ void slab(const NsSmall& p, const NsOut& o, int b, int c0, int c1,
@@ -239,14 +240,33 @@ __device__ __forceinline__ void slab(const NsSmall& p, const NsOut& o, int b, in
     }
     if constexpr (MODE != kApplyOut) {
         const float mul = pow2(-2 * (MODE == kGram ? ex : ex2));
+        if constexpr (S::kSplit > 1) {
+            // the shares of a tile, added in order by the last one's wave
+            float* share = (float*)C;
+            const int tile = wave / S::kSplit, ks = wave % S::kSplit;
+            if (tile < S::kTiles && ks + 1 < S::kSplit)
+#pragma unroll
+                for (int q = 0; q < 16; ++q)
+                    share[(wave * 16 + q) * 64 + lane] = hi[0][q] + lo[0][q];
+            __syncthreads();
+            if (tile < S::kTiles && ks + 1 == S::kSplit)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    float s = 0.f;
+#pragma unroll
+                    for (int w = 1; w < S::kSplit; ++w)
+                        s += share[((wave - w) * 16 + q) * 64 + lane];
+                    hi[0][q] += s;
+                }
+        }
 #pragma unroll
         for (int o2 = 0; o2 < S::kOwn; ++o2) {
             const int unit = wave + kWaves * o2;
-            if (unit < S::kTiles * S::kSplit) {
-                const int tile = unit / S::kSplit, ks = unit % S::kSplit;
+            if (unit < S::kTiles * S::kSplit && unit % S::kSplit + 1 == S::kSplit) {
+                const int tile = unit / S::kSplit;
                 const int I = tile >= 6 ? 3 : (tile >= 3 ? 2 : (tile >= 1 ? 1 : 0));
                 const int J = tile - I * (I + 1) / 2;
-                float* out = p.part + ((size_t)b * p.parts + slab_no * S::kSplit + ks) * S::LD * S::LD;
+                float* out = p.part + ((size_t)b * p.parts + slab_no) * S::LD * S::LD;
 #pragma unroll
                 for (int q = 0; q < 16; ++q) {
                     const int i = 32 * I + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3);
@@ -273,25 +293,26 @@ __device__ __forceinline__ void segment(const NsSmall& p, const NsSteps& st, int
     if (live) {
         const float* src = p.part + (size_t)b * p.parts * S::LD * S::LD;
 #pragma unroll
-        for (int I = 0; I < S::T16; ++I) {
-            const int i = 16 * I + 4 * g;
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int q = 0; q < parts; ++q) {
-                const float* s = src + (size_t)q * S::LD * S::LD;
+        for (int I = 0; I < S::T16; ++I)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                R[I][e] = 0.f;
+        for (int q = 0; q < parts; ++q) {
+            const float* s = src + (size_t)q * S::LD * S::LD;
+#pragma unroll
+            for (int I = 0; I < S::T16; ++I) {
+                const int i = 16 * I + 4 * g;
                 if (I >= (wave & ~1)) {  // 32-block I / 2 of the rows at or below the panel's
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        v[e] += s[(i + e) * S::LD + j];
+                        R[I][e] += s[(i + e) * S::LD + j];
                 } else {
                     const floatx4 x = *(const floatx4*)(s + j * S::LD + i);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        v[e] += x[e];
+                        R[I][e] += x[e];
                 }
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                R[I][e] = v[e];
         }
     }
     for (int l = 0; l < L; ++l) {
@@ -359,18 +380,30 @@ ns_slab_kernel(const NsSmall p, const NsOut o, int from_u, int ex, int ep, int e
                         p.p_img + (size_t)b * Small<MT>::kImage, lds);
 }
 
-// The parts summed in order into the first.
+// The parts summed in order into the first: 64 elements to a workgroup, a
+// fourth of the parts to each of its waves, eight loads in flight.
 __global__ void __launch_bounds__(256)
 ns_parts_kernel(float* part, int parts, int size)
 {
+    __shared__ float sum[4][64];
     float* p = part + (size_t)blockIdx.y * parts * size;
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= size)
-        return;
+    const int i = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+    const int q0 = parts * w / 4, q1 = parts * (w + 1) / 4;
     float s = 0.f;
-    for (int q = 0; q < parts; ++q)
-        s += p[(size_t)q * size + i];
-    p[i] = s;
+    for (int q = q0; q < q1; q += 8) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = q + e < q1 ? p[(size_t)(q + e) * size + i] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            s += v[e];
+    }
+    sum[w][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (w == 0)
+        p[i] = (sum[0][threadIdx.x] + sum[1][threadIdx.x]) +
+               (sum[2][threadIdx.x] + sum[3][threadIdx.x]);
 }
 
 template <int MT>
@@ -392,10 +425,30 @@ ns_solo_kernel(const NsSmall p, const NsSteps st, const NsOut o)
     const int b = blockIdx.x;
     const int64_t base = (int64_t)b * p.in.count;
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < p.in.count; i += kThreads) {
-        float u[1];
-        load_u<1>(p.in, base + i, true, u);
-        s += (double)u[0] * (double)u[0];
+    constexpr int B = 16;  // loads in flight
+    for (int64_t i0 = threadIdx.x; i0 < p.in.count; i0 += kThreads * B) {
+        float u[B][1], v[B];
+#pragma unroll
+        for (int e = 0; e < B; ++e) {
+            const int64_t i = i0 + e * kThreads;
+            u[e][0] = v[e] = 0.f;
+            if (i < p.in.count) {
+                load_vec<1>(p.in, base + i, u[e]);
+                if (p.in.v)
+                    v[e] = p.in.v[base + i];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < B; ++e) {
+            const int64_t i = i0 + e * kThreads;
+            if (p.in.v) {
+                v[e] = p.in.mu * v[e] + u[e][0];
+                if (i < p.in.count)
+                    p.in.v[base + i] = v[e];
+                u[e][0] = p.in.nesterov ? u[e][0] + p.in.mu * v[e] : v[e];
+            }
+            s += (double)u[e][0] * (double)u[e][0];
+        }
     }
     const double inv = inv_from(block_sum<kWaves>(s), p.eps);
     __syncthreads();
@@ -404,7 +457,7 @@ ns_solo_kernel(const NsSmall p, const NsSteps st, const NsOut o)
     for (int seg = 0; seg < st.segments; ++seg) {
         const int L = st.length[seg];
         __syncthreads();
-        segment<MT>(p, st, b, k, L, S::kSplit, lds, lds);
+        segment<MT>(p, st, b, k, L, 1, lds, lds);
         k += L;
         __syncthreads();
         const int ep = st.ep[k - 1];
@@ -435,11 +488,11 @@ hipError_t launch(const NsPlan& q, const NsSmall& p, const NsSteps& st, const Ns
     for (int seg = 0; seg < q.segments; ++seg) {
         const int L = q.length[seg];
         int parts = p.parts;
-        // one workgroup reads 100 GB/s or so: above 256 KB a launch that sums
-        // the parts first costs less
-        if ((size_t)parts * S::LD * S::LD * 4 > (256 << 10)) {
+        // the one workgroup reads a part in a microsecond or two: beyond four, a
+        // launch that sums them first costs less
+        if (parts > 4) {
             hipLaunchKernelGGL(ns_parts_kernel,
-                               dim3((unsigned)(S::LD * S::LD / 256), (unsigned)q.batch), dim3(256),
+                               dim3((unsigned)(S::LD * S::LD / 64), (unsigned)q.batch), dim3(256),
                                0, s, p.part, parts, S::LD * S::LD);
             parts = 1;
         }
@@ -462,9 +515,11 @@ void ns_small_sizes(int m, int n, NsPlan* q)
 {
     const int mt = (m + 31) / 32;
     q->chunks = (n + kChunk - 1) / kChunk;
-    q->solo = q->chunks <= kNsSoloChunks;
+    // everything in one launch against a launch per part, us: 32 x 300 25 / 35,
+    // 64 x 128 30 / 40, 96 x 128 61 / 75, but 64 x 512 61 / 43, 128 x 512 181 / 94
+    q->solo = q->chunks <= (mt == 1 ? 4 : 1);
     q->slabs = q->solo ? 1 : std::min(q->chunks, 64);
-    q->parts = q->slabs * (mt == 1 ? 8 : (mt == 2 ? 2 : 1));
+    q->parts = q->slabs;
     q->part_bytes = (size_t)q->parts * mt * mt * 4096;
     q->img_bytes = (size_t)32 * mt * (mt * 128 + 16);
     q->xs_bytes = (size_t)q->chunks * kChunk * mt * 128;
