@@ -537,10 +537,26 @@ def newton_schulz_workspace_size(desc):
     return n.value
 
 
-def _same_device(first, *others):
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError("tensors are on different devices")
+def _checked(device, t, name, dtype):
+    """t is a contiguous tensor of dtype on device (None passes)."""
+    if t is not None and not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and
+                              t.device == device):
+        _dev(t, name, dtype)
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _call(device, fn, *args, stream=None):
+    """fn(*args, stream) with `device` current, on `stream` or its current one."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _call(device, fn, *args, stream=stream)
+    raw = (torch._C._cuda_getCurrentRawStream(device.index) if stream is None
+           else stream.cuda_stream)
+    check(fn(*args, raw))
 
 
 def newton_schulz(g, steps=5, coef=NS_COEF, eps=1e-7, group=1, out=None, ws=None, stream=None):
@@ -553,14 +569,13 @@ def newton_schulz(g, steps=5, coef=NS_COEF, eps=1e-7, group=1, out=None, ws=None
                 CAFFE_BF16 if g.dtype == torch.bfloat16 else CAFFE_F32)
     if out is None:
         out = torch.empty_like(g)
-    _dev(out, "out", g.dtype)
+    _checked(g.device, out, "out", g.dtype)
     if out.shape != g.shape:
         raise ValueError("in and out differ in shape")
-    _same_device(g, out)
-    with torch.cuda.device(g.device):
-        buf = (ws or Workspace(g.device)).get(newton_schulz_workspace_size(d))
-        check(load().caffe_newton_schulz(ctypes.byref(d), _ptr(g), _ptr(out), _ptr(buf),
-                                         0 if buf is None else buf.numel(), _stream(stream)))
+    buf = (ws or Workspace(g.device)).get(newton_schulz_workspace_size(d))
+    _checked(g.device, buf, "workspace", torch.uint8)
+    _call(g.device, load().caffe_newton_schulz, ctypes.byref(d), g.data_ptr(), out.data_ptr(),
+          _addr(buf), 0 if buf is None else buf.numel(), stream=stream)
     return out
 
 
@@ -570,40 +585,44 @@ def muon_update(w, g, v, lr, momentum=0.95, weight_decay=0.0, nesterov=True, sca
     w <- w - lr (scale newton_schulz(u) + weight_decay w).  `scale` defaults to
     sqrt(max(1, rows / cols)).  `lr` is a number, or a one-element float32
     device tensor read when the kernel runs (for graph capture)."""
-    for t, n in ((w, "w"), (g, "g"), (v, "v")):
-        _dev(t, n, torch.float32)
+    _dev(w, "w", torch.float32)
+    dev = w.device
+    _checked(dev, g, "g", torch.float32), _checked(dev, v, "v", torch.float32)
     if not (w.shape == g.shape == v.shape):
         raise ValueError("w, g and v must have the same shape")
     d = ns_desc(w.shape, steps, coef, eps, group)
     if scale is None:
         scale = max(1.0, d.rows / max(1, d.cols)) ** 0.5
-    lib = load()
-    _same_device(w, g, v, lr if isinstance(lr, torch.Tensor) else None)
-    with torch.cuda.device(w.device):
-        buf = (ws or Workspace(w.device)).get(newton_schulz_workspace_size(d))
-        tail = (float(momentum), float(weight_decay), float(scale), int(bool(nesterov)),
-                _ptr(buf), 0 if buf is None else buf.numel(), _stream(stream))
-        if isinstance(lr, torch.Tensor):
-            _dev(lr, "lr", torch.float32)
-            if lr.numel() != 1:
-                raise ValueError("lr must have one element")
-            check(lib.caffe_muon_update_device_lr(ctypes.byref(d), _ptr(w), _ptr(g), _ptr(v),
-                                                  _ptr(lr), *tail))
-        else:
-            check(lib.caffe_muon_update(ctypes.byref(d), _ptr(w), _ptr(g), _ptr(v), float(lr),
-                                        *tail))
+    buf = (ws or Workspace(dev)).get(newton_schulz_workspace_size(d))
+    _checked(dev, buf, "workspace", torch.uint8)
+    on_device = isinstance(lr, torch.Tensor)
+    if on_device:
+        _checked(dev, lr, "lr", torch.float32)
+        if lr.numel() != 1:
+            raise ValueError("lr must have one element")
+    _call(dev, load().caffe_muon_update_device_lr if on_device else load().caffe_muon_update,
+          ctypes.byref(d), w.data_ptr(), g.data_ptr(), v.data_ptr(),
+          lr.data_ptr() if on_device else float(lr), float(momentum), float(weight_decay),
+          float(scale), int(bool(nesterov)), _addr(buf), 0 if buf is None else buf.numel(),
+          stream=stream)
 
 
 # ------------------------------------------------------------- 8-bit rows
 def int8_pitch(cols):
-    """Bytes between 8-bit rows of `cols` values."""
-    p = load().caffe_int8_pitch(int(cols))
-    if p == 0:
+    """Bytes between 8-bit rows of `cols` values (caffe_int8_pitch)."""
+    if not 1 <= cols <= 1 << 17:
         raise ValueError(f"8-bit rows hold 1 to 2^17 values, not {cols}")
-    return p
+    return (int(cols) + 127) // 128 * 128
 
 
 _ROW_TYPES = {torch.float32: CAFFE_F32, torch.bfloat16: CAFFE_BF16}
+
+
+def _row_values(x):
+    n = 1
+    for v in x.shape[1:]:
+        n *= v
+    return n
 
 
 def quantize_rows(x, q=None, scale=None, stream=None):
@@ -615,19 +634,17 @@ def quantize_rows(x, q=None, scale=None, stream=None):
     _dev(x, "x", x.dtype)
     if x.dim() < 2:
         raise ValueError("x must have rows and columns")
-    rows, cols = x.shape[0], x[0].numel() if x.shape[0] else int(torch.tensor(x.shape[1:]).prod())
+    dev, rows, cols = x.device, x.shape[0], _row_values(x)
     pitch = int8_pitch(cols)
     if q is None:
-        q = torch.empty((rows, pitch), dtype=torch.int8, device=x.device)
+        q = torch.empty((rows, pitch), dtype=torch.int8, device=dev)
     if scale is None:
-        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
-    _dev(q, "q", torch.int8), _dev(scale, "scale", torch.float32)
-    if tuple(q.shape) != (rows, pitch) or scale.numel() != rows:
+        scale = torch.empty(rows, dtype=torch.float32, device=dev)
+    _checked(dev, q, "q", torch.int8), _checked(dev, scale, "scale", torch.float32)
+    if q.shape != (rows, pitch) or scale.numel() != rows:
         raise ValueError(f"q must be {(rows, pitch)} and scale {(rows,)}")
-    _same_device(x, q, scale)
-    with torch.cuda.device(x.device):
-        check(load().caffe_quantize_rows(_ptr(x), _ROW_TYPES[x.dtype], rows, cols, _ptr(q),
-                                         _ptr(scale), _stream(stream)))
+    _call(dev, load().caffe_quantize_rows, x.data_ptr(), _ROW_TYPES[x.dtype], rows, cols,
+          q.data_ptr(), scale.data_ptr(), stream=stream)
     return q, scale
 
 
@@ -640,17 +657,16 @@ def inner_product_int8(x, weight, weight_scale, bias=None, C=None, x_scale=None,
     rows8 = x.dtype == torch.int8
     if not rows8 and x.dtype not in _ROW_TYPES:
         raise ValueError(f"bottom must be float32, bfloat16 or int8, got {x.dtype}")
-    _dev(x, "bottom", x.dtype), _dev(weight, "weight", torch.int8)
-    _dev(weight_scale, "weight_scale", torch.float32), _dev(bias, "bias", torch.float32)
-    _dev(x_scale, "bottom_scale", torch.float32)
     if top_dtype not in _ROW_TYPES:
         raise ValueError(f"top must be float32 or bfloat16, got {top_dtype}")
-    N = x.shape[0]
+    _dev(x, "bottom", x.dtype)
+    dev = x.device
+    _checked(dev, weight, "weight", torch.int8)
+    for t, name in ((weight_scale, "weight_scale"), (bias, "bias"), (x_scale, "bottom_scale")):
+        _checked(dev, t, name, torch.float32)
     if x.dim() < 2 or weight.dim() != 2:
         raise ValueError("bottom must have rows, weight (K, pitch)")
-    per = 1
-    for v in x.shape[1:]:
-        per *= int(v)
+    N, per = x.shape[0], _row_values(x)
     if C is None:
         if rows8:
             raise ValueError("8-bit rows need C, the values of a row")
@@ -664,19 +680,20 @@ def inner_product_int8(x, weight, weight_scale, bias=None, C=None, x_scale=None,
     if weight_scale.numel() != K or (bias is not None and bias.numel() != K):
         raise ValueError(f"weight_scale and bias must have K={K} elements")
     if out is None:
-        out = torch.empty((N, K), dtype=top_dtype, device=x.device)
-    _dev(out, "top", top_dtype)
+        out = torch.empty((N, K), dtype=top_dtype, device=dev)
+    _checked(dev, out, "top", top_dtype)
     if out.numel() != N * K:
         raise ValueError(f"top must have {N} x {K} elements")
-    _same_device(x, weight, weight_scale, bias, x_scale, out)
     d = Ip8Desc(N, int(C), K, int(bool(relu)), CAFFE_INT8_ROWS if rows8 else _ROW_TYPES[x.dtype],
                 _ROW_TYPES[top_dtype])
     lib = load()
-    with torch.cuda.device(x.device):
+    desc, buf = ctypes.byref(d), None
+    if not rows8:
         n = ctypes.c_size_t()
-        check(lib.caffe_inner_product_int8_workspace_size(ctypes.byref(d), ctypes.byref(n)))
-        buf = (ws or Workspace(x.device)).get(n.value)
-        check(lib.caffe_inner_product_int8(
-            ctypes.byref(d), _ptr(x), _ptr(x_scale), _ptr(weight), _ptr(weight_scale), _ptr(bias),
-            _ptr(out), _ptr(buf), 0 if buf is None else buf.numel(), _stream(stream)))
+        check(lib.caffe_inner_product_int8_workspace_size(desc, ctypes.byref(n)))
+        buf = (ws or Workspace(dev)).get(n.value)
+        _checked(dev, buf, "workspace", torch.uint8)
+    _call(dev, lib.caffe_inner_product_int8, desc, x.data_ptr(), _addr(x_scale),
+          weight.data_ptr(), weight_scale.data_ptr(), _addr(bias), out.data_ptr(), _addr(buf),
+          0 if buf is None else buf.numel(), stream=stream)
     return out

@@ -14,24 +14,50 @@ namespace {
 
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 
-// The whole number next to x / s, halves to the even one, exactly: the
-// rounded quotient t = fl(x / s) lies on the same side of every half as x / s
-// or on the half itself, and then the remainder x - t s (exact in one fma)
-// says on which side the quotient was.
-__device__ __forceinline__ int round_quotient(float x, float s)
+// The whole number next to x / s, halves to the even one, exactly.  x * inv,
+// inv = fl(1 / s), is within 127 * 2^-23 < 2^-16 of the quotient, so its
+// rounding is the quotient's unless it lies within 2^-15 of a half.  There the
+// rounded quotient t = fl(x / s) decides: it is on the same side of the half as
+// x / s, or on the half itself, and then the remainder x - t s (exact in one
+// fma) says on which side the quotient was.
+__device__ __forceinline__ int round_quotient(float x, float s, float inv)
 {
-    const float t = x / s;
-    float r = rintf(t);
-    const float d = t - r;  // exact
-    if (fabsf(d) == 0.5f) {
-        const float rem = fmaf(-t, s, x);
-        // toward the side of the quotient (s > 0); the even one at rem = 0
-        if (rem > 0.f && d > 0.f)
-            r += 1.f;
-        else if (rem < 0.f && d < 0.f)
-            r -= 1.f;
+    const float near = x * inv;
+    float r = rintf(near);
+    if (!(fabsf(fabsf(near - r) - 0.5f) > 0x1p-15f)) {  // (also where inv overflows)
+        const float t = x / s;
+        r = rintf(t);
+        const float d = t - r;  // exact
+        if (fabsf(d) == 0.5f) {
+            const float rem = fmaf(-t, s, x);
+            // toward the side of the quotient (s > 0); the even one at rem = 0
+            if (rem > 0.f && d > 0.f)
+                r += 1.f;
+            else if (rem < 0.f && d < 0.f)
+                r -= 1.f;
+        }
     }
     return (int)fminf(fmaxf(r, -127.f), 127.f);
+}
+
+// A row's scale from its largest absolute value's bits: NaN if that is not a
+// number or infinite.
+__device__ __forceinline__ float row_scale(uint32_t top)
+{
+    return top >= 0x7F800000u ? NAN : __builtin_bit_cast(float, top) / 127.f;
+}
+
+// four values as 8-bit numbers (zeros unless the scale is positive)
+__device__ __forceinline__ uint32_t round_row4(const float (&x)[4], float s)
+{
+    uint32_t w = 0;
+    if (s > 0.f) {
+        const float inv = 1.f / s;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            w |= (uint32_t)(uint8_t)round_quotient(x[e], s, inv) << (8 * e);
+    }
+    return w;
 }
 
 template <typename T, int VEC>
@@ -71,12 +97,12 @@ __device__ __forceinline__ void load4(const T* p, int left, float (&x)[4])
 // LANES threads take a row, each CH chunks of four kept in registers; longer
 // rows are read again.  Bound by HBM.
 template <typename T, int VEC, int LANES, int CH>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(LANES > 256 ? LANES : 256)
 quantize_rows_kernel(const T* __restrict__ x, int64_t rows, int cols, int pitch,
                      int8_t* __restrict__ q, float* __restrict__ scale)
 {
-    constexpr int RPB = 256 / LANES;
-    __shared__ uint32_t part[4];
+    constexpr int RPB = LANES > 256 ? 1 : 256 / LANES;
+    __shared__ uint32_t part[LANES > 64 ? LANES / 64 : 1];
     const int lane = threadIdx.x % LANES;
     const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / LANES;
     const bool live = row < rows;
@@ -105,25 +131,17 @@ quantize_rows_kernel(const T* __restrict__ x, int64_t rows, int cols, int pitch,
         if ((threadIdx.x & 63) == 0)
             part[threadIdx.x >> 6] = top;
         __syncthreads();
-        top = max(max(part[0], part[1]), max(part[2], part[3]));
+#pragma unroll
+        for (int w = 0; w < LANES / 64; ++w)
+            top = max(top, part[w]);
     }
     if (!live)
         return;
-    const bool bad = top >= 0x7F800000u;
-    const float s = bad ? NAN : __builtin_bit_cast(float, top) / 127.f;
-    const bool some = s > 0.f;
+    const float s = row_scale(top);
     if (lane == 0)
         scale[row] = s;
     int8_t* o = q + row * (int64_t)pitch;
-    auto put = [&](int c, const float(&y)[4]) {
-        uint32_t w = 0;
-        if (some) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                w |= (uint32_t)(uint8_t)round_quotient(y[e], s) << (8 * e);
-        }
-        *(uint32_t*)(o + c) = w;
-    };
+    auto put = [&](int c, const float(&y)[4]) { *(uint32_t*)(o + c) = round_row4(y, s); };
 #pragma unroll
     for (int h = 0; h < CH; ++h) {
         const int c = (h * LANES + lane) * 4;
@@ -141,7 +159,11 @@ template <typename T, int VEC>
 void quantize_rows(const T* x, int64_t rows, int cols, int pitch, int8_t* q, float* scale,
                    hipStream_t s)
 {
-    if (cols <= 1024)
+    // few long rows: a thousand threads to each (20 x 9216: 6.5 us with 256)
+    if (rows <= 512 && cols > 1024)
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_rows_kernel<T, VEC, 1024, 4>),
+                           dim3((unsigned)rows), dim3(1024), 0, s, x, rows, cols, pitch, q, scale);
+    else if (cols <= 1024)
         hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_rows_kernel<T, VEC, 64, 4>),
                            dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, x, rows, cols, pitch,
                            q, scale);
@@ -169,7 +191,10 @@ __device__ __forceinline__ float ip8_finish(int acc, float s, float t, float bia
     return z > 0.f ? z : (relu ? 0.f : z);
 }
 
-typedef TileNT<OpInt8, 2, 2, 1, 1, 3, false> Ip8Tile64;
+// 64 x 64 and 128 x 128 by four waves, 256 x 256 by eight
+typedef TileNT<OpInt8Line, 2, 2, 1, 1, 5, false> Ip8Tile64;
+typedef TileNT<OpInt8Line, 2, 2, 2, 2, 2, false> Ip8Tile128;
+typedef TileNT<OpInt8Half, 4, 2, 2, 4, 2, false> Ip8Tile256;
 
 template <class Tile>
 __global__ void __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd)
@@ -188,21 +213,36 @@ ip8_tile_kernel(const Ip8Params p)
     Tile::run(p.x + (size_t)m0 * p.pitch, (uint32_t)min(Tile::TM, p.N - m0) * p.pitch, p.pitch,
               p.w + (size_t)n0 * p.pitch, (uint32_t)min(Tile::TN, p.K - n0) * p.pitch, p.pitch, 0,
               (int)(p.pitch / 128), acc);
+    const bool vec = p.K % 4 == 0;
     Tile::each(acc, [&](int di, int dj, int(&v)[4]) {
-        const int i = m0 + di, j = n0 + dj;
-        if (j >= p.K)
+        const int i = m0 + di, j = n0 + dj, jc = min(j, p.K - 1);
+        const float t = p.ws[jc], bias = p.bias ? p.bias[jc] : 0.f;
+        float z[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            z[e] = ip8_finish(v[e], p.xs[min(i + e, p.N - 1)], t, bias, p.relu);
+        if (vec) {  // four outputs of a sample to a lane
+            quad_transpose(z);
+            const int n = i + (threadIdx.x & 3), k = j - (threadIdx.x & 3);
+            if (n >= p.N || k >= p.K)
+                return;
+            const size_t at = (size_t)n * p.K + k;
+            if (p.out_bf16)
+                *(u32x2*)(p.out_bf16 + at) = u32x2{f32x2_to_bf16x2_rne(z[0], z[1]),
+                                                   f32x2_to_bf16x2_rne(z[2], z[3])};
+            else
+                *(floatx4*)(p.out_f32 + at) = floatx4{z[0], z[1], z[2], z[3]};
             return;
-        const float t = p.ws[j], bias = p.bias ? p.bias[j] : 0.f;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (i + e >= p.N)
+            if (i + e >= p.N || j >= p.K)
                 continue;
-            const float z = ip8_finish(v[e], p.xs[i + e], t, bias, p.relu);
             const size_t at = (size_t)(i + e) * p.K + j;
             if (p.out_bf16)
-                p.out_bf16[at] = f32_to_bf16_rne(z);
+                p.out_bf16[at] = f32_to_bf16_rne(z[e]);
             else
-                p.out_f32[at] = z;
+                p.out_f32[at] = z[e];
         }
     });
 }
@@ -215,6 +255,126 @@ hipError_t launch_ip8_tile(const Ip8Params& p, hipStream_t s)
     hipLaunchKernelGGL(HIP_KERNEL_NAME(ip8_tile_kernel<Tile>),
                        dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(Tile::kThreads), 0, s, p);
     return hipGetLastError();
+}
+
+// A few samples: the stream of the weights.  A workgroup takes 16 outputs, its
+// eight waves a share of the reduction each, 64 bytes of every weight row to a
+// step of the 16x16x64 instruction straight from memory (lane l: row l % 16,
+// bytes 16 (l / 16) ..), and the shares are added in LDS.  QUANT (one sample of at most kQuantRow values): the workgroup
+// brings the float sample to 8 bits itself, while its first weights are on
+// their way; otherwise 8-bit rows are read as the weights are.
+constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves;
+constexpr int kQuantRow = 16384;
+constexpr int kFewSamples = 16;  // (a tile of 64 is as fast at 20: 4096 x 9216 15.6 / 15.9 us)
+
+template <typename T, int VEC, bool QUANT>
+__global__ void __launch_bounds__(kFewThreads)
+ip8_few_kernel(const Ip8Params p, const T* __restrict__ xf, int C)
+{
+    constexpr int U = 8;  // steps in flight
+    __shared__ u32x4 xq[QUANT ? kQuantRow / 16 : 1];
+    __shared__ uint32_t top[kFewWaves];
+    float xscale = 0.f;
+    __shared__ int sum[kFewWaves][256];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int k0 = blockIdx.x * 16;
+    const int steps = (int)(p.pitch / 64);
+    const int t0 = steps * wave / kFewWaves, t1 = steps * (wave + 1) / kFewWaves;
+    // rows past the last re-read it: their results are not stored
+    const int8_t* w = p.w + (size_t)min(k0 + r, p.K - 1) * p.pitch + g * 16;
+    const int8_t* x = p.x + (size_t)min(r, p.N - 1) * p.pitch + g * 16;
+    intx4 acc = {0, 0, 0, 0};
+    intx4 wv[U], xv[U];
+    auto load = [&](int t) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = min(t + u, steps - 1) * 64;
+            wv[u] = *(const intx4*)(w + c);
+            if constexpr (!QUANT)
+                xv[u] = *(const intx4*)(x + c);
+        }
+    };
+    load(t0);
+    if constexpr (QUANT) {
+        constexpr int CH = kQuantRow / (kFewThreads * 4);
+        float y[CH][4];
+        uint32_t m = 0;
+#pragma unroll
+        for (int h = 0; h < CH; ++h) {
+            const int c = (h * kFewThreads + (int)threadIdx.x) * 4;
+            load4<T, VEC>(xf + c, C - c, y[h]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                m = max(m, __builtin_bit_cast(uint32_t, y[h][e]) & 0x7FFFFFFFu);
+        }
+        for (int off = 32; off > 0; off >>= 1)
+            m = max(m, (uint32_t)__shfl_xor((int)m, off, 64));
+        if (lane == 0)
+            top[wave] = m;
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < kFewWaves; ++v)
+            m = max(m, top[v]);
+        xscale = row_scale(m);
+#pragma unroll
+        for (int h = 0; h < CH; ++h) {
+            const int c = (h * kFewThreads + (int)threadIdx.x) * 4;
+            if (c < (int)p.pitch)
+                ((uint32_t*)xq)[c / 4] = round_row4(y[h], xscale);
+        }
+        __syncthreads();
+    }
+    for (int t = t0; t < t1; t += U) {
+        if (t > t0)
+            load(t);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if constexpr (QUANT) {
+                xv[u] = intx4{0, 0, 0, 0};
+                if (r == 0 && t + u < t1)
+                    xv[u] = __builtin_bit_cast(intx4, xq[(t + u) * 4 + g]);
+            }
+            if (t + u < t1)
+                acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(xv[u], wv[u], acc, 0, 0, 0);
+        }
+    }
+    // lane l holds samples 4 g + q of output l % 16
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        sum[wave][(4 * g + q) * 16 + r] = acc[q];
+    __syncthreads();
+    const int i = threadIdx.x, n = i >> 4, k = k0 + (i & 15);
+    if (n < p.N && k < p.K) {
+        int s = 0;
+#pragma unroll
+        for (int v = 0; v < kFewWaves; ++v)
+            s += sum[v][i];
+        const float z = ip8_finish(s, QUANT ? xscale : p.xs[n], p.ws[k],
+                                   p.bias ? p.bias[k] : 0.f, p.relu);
+        const size_t at = (size_t)n * p.K + k;
+        if (p.out_bf16)
+            p.out_bf16[at] = f32_to_bf16_rne(z);
+        else
+            p.out_f32[at] = z;
+    }
+}
+
+template <typename T, int VEC, bool QUANT>
+hipError_t launch_ip8_few(const Ip8Params& p, const void* x, int C, hipStream_t s)
+{
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ip8_few_kernel<T, VEC, QUANT>),
+                       dim3((unsigned)((p.K + 15) / 16)), dim3(kFewThreads), 0, s, p,
+                       (const T*)x, C);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_ip8_quant(const Ip8Params& p, const void* x, int C, hipStream_t s)
+{
+    return C % 4 == 0 ? launch_ip8_few<T, 4, true>(p, x, C, s)
+                      : launch_ip8_few<T, 1, true>(p, x, C, s);
 }
 
 }  // namespace
@@ -252,6 +412,9 @@ hipError_t launch_inner_product_int8(const Ip8Args& a, char* ws, hipStream_t s)
     p.K = a.K;
     p.relu = a.relu;
     p.pitch = (uint32_t)a.pitch;
+    if (a.bottom_type != kIp8BottomInt8 && a.N == 1 && a.pitch <= kQuantRow)
+        return a.bottom_type == kIp8BottomBf16 ? launch_ip8_quant<uint16_t>(p, a.bottom, a.C, s)
+                                               : launch_ip8_quant<float>(p, a.bottom, a.C, s);
     if (a.bottom_type == kIp8BottomInt8) {
         p.x = (const int8_t*)a.bottom;
         p.xs = a.bottom_scale;
@@ -265,6 +428,26 @@ hipError_t launch_inner_product_int8(const Ip8Args& a, char* ws, hipStream_t s)
         p.x = q;
         p.xs = qs;
     }
+    if (a.N <= kFewSamples)
+        return launch_ip8_few<float, 1, false>(p, nullptr, a.C, s);
+    // The tile by a model of the time on 256 compute units, us: a launch and its
+    // epilogue, and per line of 128 values `one` while every unit has at most
+    // one tile, else `each` for each tile of the fullest.  Measured / modelled:
+    //        64 x 4096 x 4096  1024 x 4096 x 4096  4096 x 4096 x 4096  8192 x 9216 x 4096
+    //   64        11 / 11            35 / 34             129 / 123          521 / 535
+    //   128       30 / 34            35 / 34              94 / 89           342 / 358
+    //   256       57 / 84            65 / 84              86 / 84           298 / 297
+    auto cost = [&](int64_t tm, int64_t tn, double over, double one, double each) {
+        const int64_t n = ((a.N + tm - 1) / tm * ((a.K + tn - 1) / tn) + 255) / 256;
+        return over + a.pitch / 128 * (n <= 1 ? one : each * (double)n);
+    };
+    const double c64 = cost(64, 64, 5.0, 0.19, 0.23);
+    const double c128 = cost(128, 128, 12.0, 0.70, 0.60);
+    const double c256 = cost(256, 256, 23.0, 1.90, 1.90);
+    if (c256 < c128 && c256 < c64)
+        return launch_ip8_tile<Ip8Tile256>(p, s);
+    if (c128 < c64)
+        return launch_ip8_tile<Ip8Tile128>(p, s);
     return launch_ip8_tile<Ip8Tile64>(p, s);
 }
 

@@ -290,8 +290,35 @@ ns_gemm_kernel(const NsGemm p)
     } else {
         const int64_t base = (int64_t)b * p.M * p.N;
         const float lr = p.w ? (p.lr_dev ? *p.lr_dev : p.lr) : 0.f;
+        // four neighbours of the output to a lane where its rows allow it
+        const bool vec = (p.transposed ? p.M : p.N) % 4 == 0;
         Tile::each(acc, [&](int di, int dj, float(&v)[4]) {
-            const int i = m0 + di, j = n0 + dj;
+            int i = m0 + di, j = n0 + dj;
+            if (vec) {
+                if (!p.transposed) {
+                    quad_transpose(v);
+                    i += lt;
+                    j -= lt;
+                }
+                if (i >= p.M || j >= p.N)
+                    return;
+                const int64_t at = base + (p.transposed ? (int64_t)j * p.M + i
+                                                        : (int64_t)i * p.N + j);
+                floatx4 o = {v[0] * p.mul, v[1] * p.mul, v[2] * p.mul, v[3] * p.mul};
+                if (p.w) {
+                    const floatx4 w = *(const floatx4*)(p.w + at);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[e] = w[e] - lr * (p.step_scale * o[e] + p.decay * w[e]);
+                    *(floatx4*)(p.w + at) = o;
+                } else if (p.out_bf16) {
+                    *(u32x2*)(p.out_bf16 + at) = u32x2{f32x2_to_bf16x2_rne(o[0], o[1]),
+                                                       f32x2_to_bf16x2_rne(o[2], o[3])};
+                } else {
+                    *(floatx4*)(p.out_f32 + at) = o;
+                }
+                return;
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (i + e >= p.M || j >= p.N)

@@ -66,6 +66,20 @@ struct OpInt8 {
     }
 };
 
+// ... the line in two steps, and in one (see OpPairLine)
+struct OpInt8Half : OpInt8 {
+    static constexpr int kSteps = 2, kFrags = 2, kProds = 2;
+    static constexpr int frag(int step, int f) { return 2 * step + f; }
+    static constexpr int fa(int i) { return i; }
+    static constexpr int fb(int i) { return i; }
+};
+struct OpInt8Line : OpInt8 {
+    static constexpr int kSteps = 1, kFrags = 4, kProds = 4;
+    static constexpr int frag(int, int f) { return f; }
+    static constexpr int fa(int i) { return i; }
+    static constexpr int fb(int i) { return i; }
+};
+
 // Slot permutation of the 8 chunks of tile row r (bits 1..3 of r), the one
 // that the bf16 convolutions' 128-byte rows use.
 __device__ __forceinline__ int line_swz(int r)
