@@ -40,7 +40,7 @@ namespace caffe_hip {
 namespace {
 
 // --------------------------------------------------------------- first pass
-constexpr int kNormBlocks = 256;  // partial sums of one matrix, at most
+constexpr int kNormBlocks = 1024;  // partial sums of one matrix, at most
 
 // The momentum update and each block's part of ||u||^2, in double (squares of
 // floats neither overflow nor vanish there).  Bound by HBM.
@@ -233,6 +233,21 @@ ns_gemm_kernel(const NsGemm p)
     const char* B = p.B[job] + b * p.b_batch + (size_t)n0 * p.b_pitch;
     const int s0 = (int)((int64_t)p.stages * split / p.splits);
     const int s1 = (int)((int64_t)p.stages * (split + 1) / p.splits);
+    // kEpiQ: R's tile, where the registers have room (a lane's in each() order),
+    // on its way during the product
+    constexpr bool PRE = EPI == kEpiQ && Tile::kMI * Tile::kNI == 1;
+    u32x2 pre[PRE ? 8 : 1];
+    if constexpr (PRE) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int j = min(n0 + (wave >> 1) * 32 + (lane & 31), p.M - 1);
+        const int i = m0 + (wave & 1) * 32 + 4 * (lane >> 5), kp = (int)(p.r_pitch / 4);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const char* r = p.R + b * p.r_batch + pair_off(p.r_pitch, j, min(i + 8 * q, kp - 4));
+            pre[2 * q] = *(const u32x2*)r;
+            pre[2 * q + 1] = *(const u32x2*)(r + 64);
+        }
+    }
     typename Tile::acc_t acc[Tile::kMI][Tile::kNI];
     Tile::run(A, (uint32_t)min(Tile::TM, p.M - m0) * p.a_pitch, p.a_pitch, B,
               (uint32_t)min(Tile::TN, p.N - n0) * p.b_pitch, p.b_pitch, s0, s1 - s0, acc);
@@ -243,12 +258,22 @@ ns_gemm_kernel(const NsGemm p)
         const int kp = (int)(p.d_pitch / 4);
         const bool mirror = I != J;
         const float mul = job ? p.mul2 : p.mul;
+        int q = -1;
         Tile::each(acc, [&](int di, int dj, float(&v)[4]) {
             const int i = m0 + di, j = n0 + dj;
             if constexpr (EPI == kEpiQ) {
                 float r[4] = {0.f, 0.f, 0.f, 0.f};
-                if (j < p.M && i < kp)
+                if constexpr (PRE) {
+                    ++q;
+                    const halfx4 h = __builtin_bit_cast(halfx4, pre[2 * q]);
+                    const halfx4 l = __builtin_bit_cast(halfx4, pre[2 * q + 1]);
+                    const bool in = j < p.M && i < kp;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        r[e] = in ? (float)h[e] + (float)l[e] : 0.f;
+                } else if (j < p.M && i < kp) {
                     load_pair4(p.R + b * p.r_batch, pair_off(p.r_pitch, j, i), r);
+                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     v[e] = ((i + e == j && j < p.M ? p.a : 0.f) + p.b * r[e] +

@@ -135,7 +135,10 @@ __device__ __forceinline__ double inv_from(double sum, double eps)
 template <int WAVES>
 __device__ __forceinline__ double inv_norm(const double* part, int parts, double eps)
 {
-    return inv_from(block_sum<WAVES>((int)threadIdx.x < parts ? part[threadIdx.x] : 0.0), eps);
+    double s = 0.0;
+    for (int i = threadIdx.x; i < parts; i += 64 * WAVES)
+        s += part[i];
+    return inv_from(block_sum<WAVES>(s), eps);
 }
 
 // ------------------------------------------- matrices with a side <= 128

@@ -26,7 +26,9 @@ from . import (BACKWARD_BOTTOM_STAGED, BACKWARD_BOTTOM_TERMS, BACKWARD_MASK_BOTT
                caffe_conv_forward, conv_desc, conv_out_shape, lrn_desc,
                conv_uses_terms, conv_workspace_preferred, conv_workspace_size, lrn_backward, lrn_forward, maxpool_backward, maxpool_forward,
                lrn_pool_backward, pool_desc, pool_lrn_forward, pool_lrn_supported, relu_backward,
-               pool_out_shape, sgd_learning_rate, sgd_update, softmax_loss)
+               pool_out_shape, sgd_learning_rate, sgd_update, softmax_loss,
+               inner_product_int8, muon_update, newton_schulz_workspace_size, ns_desc,
+               quantize_rows)
 
 
 class ConvStack:
@@ -226,6 +228,8 @@ class ConvStack:
                                              p.get("pad", 0))
                 lst["lrn_desc"] = lrn_desc(pst["y"].shape, r["size"], r["alpha"], r["beta"],
                                            r["k"])
+        # (q, scale) of the layers held in 8 bits (quantize_inner_products)
+        self.int8 = [None] * n
         # when a list, (tag, event) pairs are recorded around every conv call:
         # tag = (kind, layer, "begin" | "end") with kind "fwd" (forward),
         # "bwd" (data gradient), "wgt" (weight and bias gradients) or "both"
@@ -233,6 +237,28 @@ class ConvStack:
         self.events = None
         # with a set of (kind, layer) keys, only those calls are marked
         self.mark_only = None
+
+    def quantize_inner_products(self):
+        """Hold the weights of the inner-product layers (1x1 images) as 8-bit
+        rows from now on: a quarter of the bytes (of float) that a forward pass
+        reads, for scoring with a trained network.  The float weights stay; a
+        call after they changed makes the rows again.  Returns the layers'
+        indices.  A network with such layers has no backward pass."""
+        need, done = 0, []
+        for l, L in enumerate(self.layers):
+            if (L.H, L.W, L.k, L.p, L.g) != (1, 1, 1, 0, 1):
+                continue
+            q, scale = self.int8[l] or (None, None)
+            self.int8[l] = quantize_rows(self.W[l].view(L.K, L.C), q, scale)
+            # its input comes in float: nothing is staged for it
+            self.bottom_staged[l] = False
+            if l > 0:
+                self.lrn_stage_only[l - 1] = False
+            need = max(need, self.N * (self.int8[l][0].shape[1] + 4))
+            done.append(l)
+        self.ws_int8 = Workspace(self.W[0].device)
+        self.ws_int8.get(need)
+        return done
 
     def _mark(self, tag, s):
         if self.events is not None and (self.mark_only is None or tag[:2] in self.mark_only):
@@ -250,8 +276,14 @@ class ConvStack:
             cur = cur.view(self.N, L.C, L.H, L.W)
             self.bottom[l] = cur
             self._mark(("fwd", l, "begin"), s)
-            caffe_conv_forward(self.descs[l], cur, self.W[l], self.b[l], self.top[l], self.ws_of[l],
-                               s, flags=FORWARD_BOTTOM_STAGED if self.bottom_staged[l] else 0)
+            if self.int8[l] is not None:
+                q, scale = self.int8[l]
+                inner_product_int8(cur.view(self.N, L.C), q, scale, self.b[l], relu=L.relu,
+                                   out=self.top[l], ws=self.ws_int8, stream=s)
+            else:
+                caffe_conv_forward(self.descs[l], cur, self.W[l], self.b[l], self.top[l],
+                                   self.ws_of[l], s,
+                                   flags=FORWARD_BOTTOM_STAGED if self.bottom_staged[l] else 0)
             self._mark(("fwd", l, "end"), s)
             cur = self.top[l]
             if self.fused[l]:
@@ -285,6 +317,8 @@ class ConvStack:
     def backward(self, top_diff, stream=None, data_grad_bottom=True):
         """top_diff: gradient w.r.t. the last top.  Fills dW, db and dbottom
         (dbottom[0] only when data_grad_bottom)."""
+        if any(q is not None for q in self.int8):
+            raise ValueError("layers held in 8 bits have no backward pass")
         s = stream or torch.cuda.current_stream()
         # (a captured graph keeps to one stream)
         capturing = torch.cuda.is_current_stream_capturing()
@@ -482,17 +516,24 @@ class SGDTrainer:
         self.net.backward(self.scores_diff, s, data_grad_bottom=False)
         return self.loss
 
-    def update(self, stream=None):
-        """One SGD step of every blob at iteration self.iter's rate."""
-        s = stream or torch.cuda.current_stream()
-        lr = sgd_learning_rate(it=self.iter, **self.schedule)
+    def _rates(self):
+        """The rates of iteration self.iter, the schedule's first."""
+        return (sgd_learning_rate(it=self.iter, **self.schedule),)
+
+    def _step(self, rates, s):
+        """One step of every blob; rates: numbers, or device tensors."""
         for l in range(len(self.net.layers)):
-            sgd_update(self.net.W[l], self.net.dW[l], self.vW[l], lr, self.momentum,
+            sgd_update(self.net.W[l], self.net.dW[l], self.vW[l], rates[0], self.momentum,
                        self.weight_decay, stream=s)
-            sgd_update(self.net.b[l], self.net.db[l], self.vb[l], lr, self.momentum,
+            sgd_update(self.net.b[l], self.net.db[l], self.vb[l], rates[0], self.momentum,
                        self.weight_decay, stream=s)
+
+    def update(self, stream=None):
+        """One step of every blob at iteration self.iter's rate."""
+        rates = self._rates()
+        self._step(rates, stream or torch.cuda.current_stream())
         self.iter += 1
-        return lr
+        return rates[0]
 
     def step(self, x, labels, stream=None):
         loss = self.forward_backward(x, labels, stream)
@@ -508,7 +549,8 @@ class SGDTrainer:
         buffer the iteration touches is preallocated and no call in it
         allocates or records a memset, so replays rerun the same launches."""
         dev = self.net.W[0].device
-        self.lr_dev = torch.empty(1, dtype=torch.float32, device=dev)
+        self.rates_dev = [torch.empty(1, dtype=torch.float32, device=dev) for _ in self._rates()]
+        self.lr_dev = self.rates_dev[0]
         # one eager pass first, so every host-side plan query happens before
         # capture (it leaves only gradients behind, which the graph rewrites)
         self.forward_backward(x, labels)
@@ -517,19 +559,50 @@ class SGDTrainer:
         with torch.cuda.graph(g):
             s = torch.cuda.current_stream()
             self.forward_backward(x, labels, s)
-            for l in range(len(self.net.layers)):
-                sgd_update(self.net.W[l], self.net.dW[l], self.vW[l], self.lr_dev, self.momentum,
-                           self.weight_decay, stream=s)
-                sgd_update(self.net.b[l], self.net.db[l], self.vb[l], self.lr_dev, self.momentum,
-                           self.weight_decay, stream=s)
+            self._step(self.rates_dev, s)
         self.graph = g
         return g
 
     def replay(self):
         """One iteration through the captured graph at iteration self.iter's
         rate (written to device memory before the replay, outside the graph)."""
-        lr = sgd_learning_rate(it=self.iter, **self.schedule)
-        self.lr_dev.fill_(lr)
+        for dst, rate in zip(self.rates_dev, self._rates()):
+            dst.fill_(rate)
         self.graph.replay()
         self.iter += 1
         return self.loss
+
+
+class MuonTrainer(SGDTrainer):
+    """SGDTrainer whose weight blobs take the orthogonalised update
+    (muon_update; each group of a convolution is a matrix of its own) and
+    whose biases take SGD.  The weights' rate is the schedule's times
+    weight_lr / base_lr; `nesterov`, `steps` and `coef` are muon_update's."""
+
+    def __init__(self, net, weight_lr=0.02, weight_momentum=0.95, weight_decay_w=0.0,
+                 nesterov=True, steps=5, coef=None, **sgd):
+        super().__init__(net, **sgd)
+        if self.schedule["base_lr"] <= 0:
+            raise ValueError("base_lr must be > 0")
+        self.weight_lr = weight_lr
+        self.weight_momentum = weight_momentum
+        self.weight_decay_w = weight_decay_w
+        self.muon = dict(nesterov=nesterov, steps=steps)
+        if coef is not None:
+            self.muon["coef"] = coef
+        # one workspace for every layer, of the largest one's size
+        self.ws = Workspace(net.W[0].device)
+        shape = {k: v for k, v in self.muon.items() if k != "nesterov"}
+        self.ws.get(max(newton_schulz_workspace_size(ns_desc(w.shape, group=L.g, **shape))
+                        for w, L in zip(net.W, net.layers)))
+
+    def _rates(self):
+        lr, = super()._rates()
+        return lr, lr * (self.weight_lr / self.schedule["base_lr"])
+
+    def _step(self, rates, s):
+        for l, L in enumerate(self.net.layers):
+            muon_update(self.net.W[l], self.net.dW[l], self.vW[l], rates[1], self.weight_momentum,
+                        self.weight_decay_w, group=L.g, ws=self.ws, stream=s, **self.muon)
+            sgd_update(self.net.b[l], self.net.db[l], self.vb[l], rates[0], self.momentum,
+                       self.weight_decay, stream=s)
