@@ -61,6 +61,13 @@ __device__ __forceinline__ void buf_st_f32(float v, __amdgpu_buffer_rsrc_t r, ui
     __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), r, byte_off, 0, 0);
 }
 
+__device__ __forceinline__ void buf_st_b128(const float (&v)[4], __amdgpu_buffer_rsrc_t r,
+                                            uint32_t byte_off)
+{
+    __builtin_amdgcn_raw_buffer_store_b128(
+        __builtin_bit_cast(u32x4, floatx4{v[0], v[1], v[2], v[3]}), r, byte_off, 0, 0);
+}
+
 // float -> bfloat16 bits, round to nearest even (a NaN stays a quiet NaN):
 // gfx950's conversion instruction, one per value or per pair.
 typedef __bf16 bf16x2_cvt __attribute__((ext_vector_type(2)));

@@ -135,7 +135,12 @@ enum NsEpi {
     kEpiQ = 1,     // D = a I + b R + c A B, symmetric, mirrored
     kEpiPart = 2,  // part[split] = A B over a share of the reduction
     kEpiX = 3,     // D = A B and its transpose D2
-    kEpiOut = 4    // the result, or the weights' step
+    // the result, or the weights' step, four neighbours of the output to a lane
+    // where its rows allow it, else one
+    kEpiOut4 = 4,
+    kEpiOut1 = 5,
+    kEpiStep4 = 6,
+    kEpiStep1 = 7
 };
 
 struct NsGemm {
@@ -146,11 +151,11 @@ struct NsGemm {
     size_t a_batch, b_batch, d_batch, d2_batch, r_batch;
     uint32_t a_pitch, b_pitch, d_pitch, d2_pitch, r_pitch;
     int M, N, stages, splits, jobs, batch;
-    float mul;     // accumulator -> the value on D's scale (kEpiQ, kEpiOut: the value itself)
+    float mul;     // accumulator -> the value on D's scale (kEpiQ, outputs: the value itself)
     float mul2;    // ... of the second product
     float a, b, c; // kEpiQ: b on R's scale
     float d_scale; // kEpiQ: value -> D's scale
-    // kEpiOut
+    // outputs
     float* out_f32;
     uint16_t* out_bf16;
     float* w;
@@ -233,20 +238,22 @@ ns_gemm_kernel(const NsGemm p)
     const char* B = p.B[job] + b * p.b_batch + (size_t)n0 * p.b_pitch;
     const int s0 = (int)((int64_t)p.stages * split / p.splits);
     const int s1 = (int)((int64_t)p.stages * (split + 1) / p.splits);
-    // kEpiQ: R's tile, where the registers have room (a lane's in each() order),
-    // on its way during the product
+    // kEpiQ: a block of R, in each()'s order; a tile of one block has it on its
+    // way during the product
     constexpr bool PRE = EPI == kEpiQ && Tile::kMI * Tile::kNI == 1;
-    u32x2 pre[PRE ? 8 : 1];
+    u32x2 pre[EPI == kEpiQ ? 8 : 1];
+    auto load_r = [&](int q, int i, int j) {
+        const char* r = p.R + b * p.r_batch +
+                        pair_off(p.r_pitch, min(j, p.M - 1), min(i, (int)(p.r_pitch / 4) - 4));
+        pre[2 * q] = *(const u32x2*)r;
+        pre[2 * q + 1] = *(const u32x2*)(r + 64);
+    };
     if constexpr (PRE) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const int j = min(n0 + (wave >> 1) * 32 + (lane & 31), p.M - 1);
-        const int i = m0 + (wave & 1) * 32 + 4 * (lane >> 5), kp = (int)(p.r_pitch / 4);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const char* r = p.R + b * p.r_batch + pair_off(p.r_pitch, j, min(i + 8 * q, kp - 4));
-            pre[2 * q] = *(const u32x2*)r;
-            pre[2 * q + 1] = *(const u32x2*)(r + 64);
-        }
+        for (int q = 0; q < 4; ++q)
+            load_r(q, m0 + (wave & 1) * 32 + 4 * (lane >> 5) + 8 * q,
+                   n0 + (wave >> 1) * 32 + (lane & 31));
     }
     typename Tile::acc_t acc[Tile::kMI][Tile::kNI];
     Tile::run(A, (uint32_t)min(Tile::TM, p.M - m0) * p.a_pitch, p.a_pitch, B,
@@ -258,22 +265,20 @@ ns_gemm_kernel(const NsGemm p)
         const int kp = (int)(p.d_pitch / 4);
         const bool mirror = I != J;
         const float mul = job ? p.mul2 : p.mul;
-        int q = -1;
-        Tile::each(acc, [&](int di, int dj, float(&v)[4]) {
+        auto load = [&](int q, int di, int dj) {
+            if constexpr (EPI == kEpiQ && !PRE)
+                load_r(q, m0 + di, n0 + dj);
+        };
+        Tile::each(acc, load, [&](int q, int di, int dj, float(&v)[4]) {
             const int i = m0 + di, j = n0 + dj;
             if constexpr (EPI == kEpiQ) {
-                float r[4] = {0.f, 0.f, 0.f, 0.f};
-                if constexpr (PRE) {
-                    ++q;
-                    const halfx4 h = __builtin_bit_cast(halfx4, pre[2 * q]);
-                    const halfx4 l = __builtin_bit_cast(halfx4, pre[2 * q + 1]);
-                    const bool in = j < p.M && i < kp;
+                const halfx4 h = __builtin_bit_cast(halfx4, pre[2 * q]);
+                const halfx4 l = __builtin_bit_cast(halfx4, pre[2 * q + 1]);
+                const bool in = j < p.M && i < kp;
+                float r[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        r[e] = in ? (float)h[e] + (float)l[e] : 0.f;
-                } else if (j < p.M && i < kp) {
-                    load_pair4(p.R + b * p.r_batch, pair_off(p.r_pitch, j, i), r);
-                }
+                for (int e = 0; e < 4; ++e)
+                    r[e] = in ? (float)h[e] + (float)l[e] : 0.f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     v[e] = ((i + e == j && j < p.M ? p.a : 0.f) + p.b * r[e] +
@@ -313,51 +318,58 @@ ns_gemm_kernel(const NsGemm p)
                 store_pair4(D, pair_off(p.d_pitch, i + lt, j - lt), v);
         });
     } else {
-        const int64_t base = (int64_t)b * p.M * p.N;
-        const float lr = p.w ? (p.lr_dev ? *p.lr_dev : p.lr) : 0.f;
-        // four neighbours of the output to a lane where its rows allow it
-        const bool vec = (p.transposed ? p.M : p.N) % 4 == 0;
-        Tile::each(acc, [&](int di, int dj, float(&v)[4]) {
-            int i = m0 + di, j = n0 + dj;
-            if (vec) {
-                if (!p.transposed) {
-                    quad_transpose(v);
-                    i += lt;
-                    j -= lt;
-                }
-                if (i >= p.M || j >= p.N)
-                    return;
-                const int64_t at = base + (p.transposed ? (int64_t)j * p.M + i
-                                                        : (int64_t)i * p.N + j);
-                floatx4 o = {v[0] * p.mul, v[1] * p.mul, v[2] * p.mul, v[3] * p.mul};
-                if (p.w) {
-                    const floatx4 w = *(const floatx4*)(p.w + at);
+        // offsets from the tile's first output fit 32 bits: 256 rows of 2^20
+        const int64_t at0 = (int64_t)b * p.M * p.N + (p.transposed ? (int64_t)n0 * p.M + m0
+                                                                   : (int64_t)m0 * p.N + n0);
+        constexpr bool STEP = EPI == kEpiStep4 || EPI == kEpiStep1;
+        constexpr bool VEC = EPI == kEpiOut4 || EPI == kEpiStep4;
+        float lr = 0.f;
+        if constexpr (STEP)
+            lr = p.lr_dev ? *p.lr_dev : p.lr;
+        const uint32_t esize = !STEP && p.out_bf16 ? 2 : 4;
+        char* out = STEP ? (char*)p.w : (p.out_bf16 ? (char*)p.out_bf16 : (char*)p.out_f32);
+        const __amdgpu_buffer_rsrc_t ro = make_rsrc(out + at0 * esize, 0x7FFFFFFFu);
+        auto off = [&](int di, int dj) -> uint32_t {
+            const uint32_t e = p.transposed ? (uint32_t)dj * p.M + di : (uint32_t)di * p.N + dj;
+            return m0 + di < p.M && n0 + dj < p.N ? e * esize : kOob;
+        };
+        const int shift = VEC && !p.transposed ? lt : 0;  // of the transposed quad
+        // the weights of a block are on their way before the first is written
+        floatx4 w[4];
+        auto load = [&](int q, int di, int dj) {
+            if constexpr (STEP && VEC)
+                w[q] = __builtin_bit_cast(floatx4, buf_ld_b128(ro, off(di + shift, dj - shift)));
+            else if constexpr (STEP)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        o[e] = w[e] - lr * (p.step_scale * o[e] + p.decay * w[e]);
-                    *(floatx4*)(p.w + at) = o;
-                } else if (p.out_bf16) {
-                    *(u32x2*)(p.out_bf16 + at) = u32x2{f32x2_to_bf16x2_rne(o[0], o[1]),
-                                                       f32x2_to_bf16x2_rne(o[2], o[3])};
-                } else {
-                    *(floatx4*)(p.out_f32 + at) = o;
-                }
-                return;
-            }
+                for (int e = 0; e < 4; ++e)
+                    w[q][e] = buf_ld_f32(ro, off(di + e, dj));
+        };
+        Tile::each(acc, load, [&](int q, int di, int dj, float(&v)[4]) {
+            if (VEC && !p.transposed)
+                quad_transpose(v);
+            float o[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (i + e >= p.M || j >= p.N)
-                    continue;
-                const int64_t at = base + (p.transposed ? (int64_t)j * p.M + i + e
-                                                        : (int64_t)(i + e) * p.N + j);
-                const float o = v[e] * p.mul;
-                if (p.w) {
-                    const float w = p.w[at];
-                    p.w[at] = w - lr * (p.step_scale * o + p.decay * w);
-                } else if (p.out_bf16) {
-                    p.out_bf16[at] = f32_to_bf16_rne(o);
-                } else {
-                    p.out_f32[at] = o;
+                o[e] = v[e] * p.mul;
+                if constexpr (STEP)
+                    o[e] = w[q][e] - lr * (p.step_scale * o[e] + p.decay * w[q][e]);
+            }
+            if constexpr (VEC) {
+                const uint32_t at = off(di + shift, dj - shift);
+                if (!STEP && p.out_bf16)
+                    __builtin_amdgcn_raw_buffer_store_b64(
+                        u32x2{f32x2_to_bf16x2_rne(o[0], o[1]), f32x2_to_bf16x2_rne(o[2], o[3])},
+                        ro, at, 0, 0);
+                else
+                    buf_st_b128(o, ro, at);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t at = off(di + e, dj);
+                    if (!STEP && p.out_bf16)
+                        __builtin_amdgcn_raw_buffer_store_b16(f32_to_bf16_rne(o[e]), ro, at, 0, 0);
+                    else
+                        buf_st_f32(o[e], ro, at);
                 }
             }
         });
@@ -426,7 +438,7 @@ hipError_t launch_gemm(const NsGemm& p, hipStream_t s)
     const double c64 = cost(tile_count<Tile64, EPI>(p), 3.5, 0.29, 0.27);
     const double c128 = cost(tile_count<Tile128, EPI>(p), 6.0, 0.90, 0.66);
     const double c192 = cost(tile_count<Tile192, EPI>(p), 12.0, 1.30, 1.30);
-    if constexpr (EPI == kEpiX || EPI == kEpiOut) {
+    if constexpr (EPI >= kEpiX) {
         const double c256 = cost(tile_count<Tile256, EPI>(p), 15.0, 1.90, 1.90);
         if (c256 < c64 && c256 < c128 && c256 < c192)
             return launch_tile<Tile256, EPI>(p, s);
@@ -738,7 +750,11 @@ hipError_t launch_newton_schulz(const NsPlan& q, const NsArgs& x, char* ws, hipS
             p.decay = x.decay;
             p.step_scale = x.step_scale;
             p.transposed = q.tall;
-            e = launch_gemm<kEpiOut>(p, s);
+            const bool four = (q.tall ? q.m : q.n) % 4 == 0;
+            if (x.w)
+                e = four ? launch_gemm<kEpiStep4>(p, s) : launch_gemm<kEpiStep1>(p, s);
+            else
+                e = four ? launch_gemm<kEpiOut4>(p, s) : launch_gemm<kEpiOut1>(p, s);
         }
         if (e != hipSuccess)
             return e;

@@ -292,10 +292,12 @@ struct TileNT {
         }
     }
 
-    // f(i, j, v): v[0..3] are rows i .. i + 3 (i a multiple of 4) of column j
-    // of the tile; lanes t = 0..3 of a quad hold columns j - t .. j - t + 3.
-    template <class F>
-    static __device__ __forceinline__ void each(const acc_t (&acc)[MI][NI], F&& f)
+    // use(q, i, j, v): v[0..3] are rows i .. i + 3 (i a multiple of 4) of column
+    // j of the tile; lanes t = 0..3 of a quad hold columns j - t .. j - t + 3.
+    // q = 0..3 of a 32 x 32 block follow one another, after load(q, i, j) of
+    // all four.
+    template <class L, class F>
+    static __device__ __forceinline__ void each(const acc_t (&acc)[MI][NI], L&& load, F&& use)
     {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -303,16 +305,29 @@ struct TileNT {
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-            for (int ni = 0; ni < NI; ++ni)
+            for (int ni = 0; ni < NI; ++ni) {
+                const int i = (wm * MI + mi) * 32 + 4 * (lane >> 5);
+                const int j = (wn * NI + ni) * 32 + (lane & 31);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    load(q, i + 8 * q, j);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     decltype(acc[0][0][0] + acc[0][0][0]) v[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         v[e] = acc[mi][ni][4 * q + e];
-                    f((wm * MI + mi) * 32 + 8 * q + 4 * (lane >> 5),
-                      (wn * NI + ni) * 32 + (lane & 31), v);
+                    use(q, i + 8 * q, j, v);
                 }
+                // (all blocks' addresses and loads at once would not fit)
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    }
+    template <class F>
+    static __device__ __forceinline__ void each(const acc_t (&acc)[MI][NI], F&& f)
+    {
+        each(acc, [](int, int, int) {},
+             [&](int, int i, int j, auto& v) { f(i, j, v); });
     }
 };
 
