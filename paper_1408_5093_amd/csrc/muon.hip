@@ -376,28 +376,76 @@ ns_gemm_kernel(const NsGemm p)
     }
 }
 
-// R = sum of the partial products, in order, as a mirrored pair matrix; the
-// parts hold the tiles of 64 below the diagonal.
+// R = sum of the partial products, in order, as a mirrored pair matrix: a
+// workgroup takes a 32 x 32 block at or below the diagonal (within the tiles of
+// 64 that the parts hold), four loads of each thread in flight, and writes it
+// and, through LDS, its mirror.
 __global__ void __launch_bounds__(256)
 ns_reduce_kernel(const float* __restrict__ part, int splits, int m, char* __restrict__ D,
                  size_t pitch, size_t d_batch, float mul)
 {
-    const int b = blockIdx.z, i = blockIdx.y;
-    const int j = (blockIdx.x * 256 + threadIdx.x) * 4;
-    if (j >= (int)(pitch / 4))
-        return;
-    const float* P = part + (size_t)b * splits * m * m;
+    __shared__ float tile[32][33];
+    int I = (int)((sqrtf(8.f * blockIdx.x + 1.f) - 1.f) * 0.5f);
+    I += ((I + 1) * (I + 2) / 2 <= (int)blockIdx.x);  // (a root rounded down)
+    I -= (I * (I + 1) / 2 > (int)blockIdx.x);         // (or up)
+    const int J = (int)blockIdx.x - I * (I + 1) / 2;
+    const int b = blockIdx.y, r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 4;
+    const int i = 32 * I + r, j = 32 * J + c;
+    const size_t size = (size_t)m * m;
+    const float* P = part + (size_t)b * splits * size;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (i < m) {
+        if (m % 4 == 0) {
+            if (j < m) {
+                const float* p = P + (size_t)i * m + j;
+                for (int s = 0; s < splits; s += 4) {
+                    floatx4 x[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        x[q] = s + q < splits ? *(const floatx4*)(p + (s + q) * size)
+                                              : floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            v[e] += x[q][e];
+                }
+            }
+        } else {
+            for (int s = 0; s < splits; s += 4) {
+                float x[4][4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[q][e] = s + q < splits && j + e < m
+                                      ? P[(s + q) * size + (size_t)i * m + j + e] : 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        v[e] += x[q][e];
+            }
+        }
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        if (j + e >= m)
-            continue;
-        const size_t at = (j >> 6) <= (i >> 6) ? (size_t)i * m + j + e : (size_t)(j + e) * m + i;
-        for (int s = 0; s < splits; ++s)
-            v[e] += P[(size_t)s * m * m + at];
         v[e] *= mul;
+        tile[r][c + e] = v[e];
     }
-    store_pair4(D + b * d_batch, pair_off(pitch, i, j), v);
+    const int kp = (int)(pitch / 4);
+    if (i < m && j < kp)
+        store_pair4(D + b * d_batch, pair_off(pitch, i, j), v);
+    if (I == J)
+        return;
+    __syncthreads();
+    const int mi = 32 * J + r, mk = 32 * I + c;  // row and columns of the mirror
+    if (mi < m && mk < kp) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] = tile[c + e][r];
+        store_pair4(D + b * d_batch, pair_off(pitch, mi, mk), v);
+    }
 }
 
 // --------------------------------------------------------------------- host
@@ -660,11 +708,10 @@ hipError_t launch_newton_schulz(const NsPlan& q, const NsArgs& x, char* ws, hipS
                 e = launch_tile<Tile64, kEpiPart>(p, s);
                 if (e != hipSuccess)
                     return e;
+                const unsigned blocks = (unsigned)((q.m + 31) / 32);
                 hipLaunchKernelGGL(ns_reduce_kernel,
-                                   dim3((unsigned)((q.m_pitch / 4 + 1023) / 1024), (unsigned)q.m,
-                                        (unsigned)q.batch),
-                                   dim3(256), 0, s, p.part, q.splits, q.m, R, q.m_pitch,
-                                   q.mm_bytes, p.mul);
+                                   dim3(blocks * (blocks + 1) / 2, (unsigned)q.batch), dim3(256),
+                                   0, s, p.part, q.splits, q.m, R, q.m_pitch, q.mm_bytes, p.mul);
                 e = hipGetLastError();
             } else {
                 e = launch_gemm<kEpiSym>(p, s);

@@ -95,6 +95,26 @@ struct Small {
 
 __device__ __forceinline__ float pow2(int e) { return ldexpf(1.f, e); }
 
+// A lane's elements (i0 + 4 g, j) of matrix b of a batch, i0 the same on all
+// lanes: byte offset at(i0) (out of range outside the matrix) + step i0.  A
+// matrix has at most 128 * 2^20 elements, so offsets fit 32 bits.
+struct Columns {
+    __amdgpu_buffer_rsrc_t r;
+    uint32_t v0, step;
+    int left;  // rows from this lane's first
+    __device__ __forceinline__ Columns(const NsSmall& p, const void* base, uint32_t esize, int b,
+                                       int j)
+        : r(make_rsrc((const char*)base + (int64_t)b * p.in.count * esize,
+                      (uint32_t)p.in.count * esize))
+    {
+        const int g4 = ((threadIdx.x & 63) >> 4) * 4;
+        v0 = (p.tall ? (uint32_t)j * p.m + g4 : (uint32_t)g4 * p.n + j) * esize;
+        step = (p.tall ? 1 : p.n) * esize;
+        left = j < p.n ? p.m - g4 : 0;
+    }
+    __device__ __forceinline__ uint32_t at(int i0) const { return i0 < left ? v0 : kOob; }
+};
+
 // Columns of X in the panels' layout: d[I][q] = X[16 I + 4 g + q][j] / norm.
 template <int MT, int VEC>
 __device__ __forceinline__ void load_columns(const NsSmall& p, int b, int j, double inv, bool from_u,
@@ -113,31 +133,57 @@ __device__ __forceinline__ void load_columns(const NsSmall& p, int b, int j, dou
         }
         return;
     }
-    const int64_t base = (int64_t)b * p.in.count;
+    // all loads of an input go out before the first is used
+    auto fetch = [&](const void* u, uint32_t esize, typename Small<MT>::Panel& x) {
+        const Columns c(p, u, esize, b, j);
 #pragma unroll
-    for (int I = 0; I < T16; ++I) {
-        const int i = 16 * I + 4 * g;
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-        if (j < p.n) {
+        for (int I = 0; I < T16; ++I) {
             if constexpr (VEC == 4) {  // tall, m % 4 == 0
-                if (i < p.m)
-                    load_u<4>(p.in, base + (int64_t)j * p.m + i, false, x);
+                if (esize == 2) {
+                    const u16x4 y = __builtin_bit_cast(
+                        u16x4, __builtin_amdgcn_raw_buffer_load_b64(c.r, c.at(16 * I), 16 * I * 2, 0));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        x[I][q] = bf16_to_f32(y[q]);
+                } else {
+                    const floatx4 y = __builtin_bit_cast(
+                        floatx4, __builtin_amdgcn_raw_buffer_load_b128(c.r, c.at(16 * I), 16 * I * 4, 0));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        x[I][q] = y[q];
+                }
             } else {
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (i + q < p.m) {
-                        float y[1];
-                        load_u<1>(p.in, base + (p.tall ? (int64_t)j * p.m + i + q
-                                                       : (int64_t)(i + q) * p.n + j),
-                                  false, y);
-                        x[q] = y[0];
-                    }
+                for (int q = 0; q < 4; ++q) {
+                    const int i = 16 * I + q;
+                    if (esize == 2)
+                        x[I][q] = bf16_to_f32(__builtin_amdgcn_raw_buffer_load_b16(
+                            c.r, c.at(i), c.step * i, 0));
+                    else
+                        x[I][q] = __builtin_bit_cast(
+                            float, __builtin_amdgcn_raw_buffer_load_b32(c.r, c.at(i), c.step * i, 0));
+                }
             }
         }
+    };
+    if (p.in.bf16)
+        fetch(p.in.g, 2, d);
+    else
+        fetch(p.in.g, 4, d);
+    if (p.in.v) {
+        typename Small<MT>::Panel h;
+        fetch(p.in.v, 4, h);
+#pragma unroll
+        for (int I = 0; I < T16; ++I)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                d[I][q] = p.in.nesterov ? d[I][q] + p.in.mu * h[I][q] : h[I][q];
+    }
+#pragma unroll
+    for (int I = 0; I < T16; ++I)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-            d[I][q] = (float)((double)x[q] * inv);
-    }
+            d[I][q] = (float)((double)d[I][q] * inv);
 }
 
 enum { kGram = 0, kApplyGram = 1, kApplyOut = 2 };
@@ -174,27 +220,45 @@ __device__ __forceinline__ void slab(const NsSmall& p, const NsOut& o, int b, in
         if constexpr (MODE != kGram) {
             S::product(P, d, pow2(ex), pow2(-ep - ex), d);
             if constexpr (MODE == kApplyOut) {
-                const int64_t base = (int64_t)b * p.in.count;
+                if (o.w) {
+                    const Columns w(p, o.w, 4, b, j);
+                    // two sixteens of rows at a time: their loads, then their stores
 #pragma unroll
-                for (int I = 0; I < S::T16; ++I) {
+                    for (int I = 0; I < S::T16; I += 2) {
+                        float x[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int i = 16 * (I + e / 4) + e % 4;
+                            x[e] = __builtin_bit_cast(
+                                float, __builtin_amdgcn_raw_buffer_load_b32(w.r, w.at(i),
+                                                                            w.step * i, 0));
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int i = 16 * (I + e / 4) + e % 4;
+                            const float y =
+                                x[e] - lr * (o.step_scale * d[I + e / 4][e % 4] + o.decay * x[e]);
+                            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, y),
+                                                                  w.r, w.at(i), w.step * i, 0);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    continue;
+                }
+                const Columns w(p, o.out_bf16 ? (const void*)o.out_bf16 : (const void*)o.out_f32,
+                                o.out_bf16 ? 2 : 4, b, j);
+#pragma unroll
+                for (int I = 0; I < S::T16; ++I)
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const int i = 16 * I + 4 * g + q;
-                        if (i >= p.m || j >= p.n)
-                            continue;
-                        const int64_t at =
-                            base + (p.tall ? (int64_t)j * p.m + i : (int64_t)i * p.n + j);
-                        if (o.w) {
-                            const float w = o.w[at];
-                            o.w[at] = w - lr * (o.step_scale * d[I][q] + o.decay * w);
-                        } else if (o.out_bf16) {
-                            o.out_bf16[at] = f32_to_bf16_rne(d[I][q]);
-                        } else {
-                            o.out_f32[at] = d[I][q];
-                        }
+                        const int i = 16 * I + q;
+                        if (o.out_bf16)
+                            __builtin_amdgcn_raw_buffer_store_b16(f32_to_bf16_rne(d[I][q]), w.r,
+                                                                  w.at(i), w.step * i, 0);
+                        else
+                            __builtin_amdgcn_raw_buffer_store_b32(
+                                __builtin_bit_cast(uint32_t, d[I][q]), w.r, w.at(i), w.step * i, 0);
                     }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
                 continue;
             }
             float* x = p.xs + ((size_t)b * p.n_pad + j) * S::LD + 4 * g;
