@@ -537,26 +537,27 @@ def newton_schulz_workspace_size(desc):
     return n.value
 
 
-def _checked(device, t, name, dtype):
-    """t is a contiguous tensor of dtype on device (None passes)."""
-    if t is not None and not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and
-                              t.device == device):
+def _checked(index, t, name, dtype):
+    """t is a contiguous tensor of dtype on device `index` (None passes)."""
+    if t is not None and not (t.dtype is dtype and t.get_device() == index and
+                              t.is_contiguous()):
         _dev(t, name, dtype)
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
+        raise ValueError(f"{name} is on {t.device}, not on device {index}")
 
 
 def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-def _call(device, fn, *args, stream=None):
-    """fn(*args, stream) with `device` current, on `stream` or its current one."""
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _call(device, fn, *args, stream=stream)
-    raw = (torch._C._cuda_getCurrentRawStream(device.index) if stream is None
-           else stream.cuda_stream)
-    check(fn(*args, raw))
+def _call(index, fn, *args, stream=None):
+    """fn(*args, stream) with device `index` current, on `stream` or its current one."""
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return _call(index, fn, *args, stream=stream)
+    status = fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None
+                else stream.cuda_stream)
+    if status:
+        check(status)
 
 
 def newton_schulz(g, steps=5, coef=NS_COEF, eps=1e-7, group=1, out=None, ws=None, stream=None):
@@ -569,12 +570,13 @@ def newton_schulz(g, steps=5, coef=NS_COEF, eps=1e-7, group=1, out=None, ws=None
                 CAFFE_BF16 if g.dtype == torch.bfloat16 else CAFFE_F32)
     if out is None:
         out = torch.empty_like(g)
-    _checked(g.device, out, "out", g.dtype)
+    dev = g.get_device()
+    _checked(dev, out, "out", g.dtype)
     if out.shape != g.shape:
         raise ValueError("in and out differ in shape")
     buf = (ws or Workspace(g.device)).get(newton_schulz_workspace_size(d))
-    _checked(g.device, buf, "workspace", torch.uint8)
-    _call(g.device, load().caffe_newton_schulz, ctypes.byref(d), g.data_ptr(), out.data_ptr(),
+    _checked(dev, buf, "workspace", torch.uint8)
+    _call(dev, load().caffe_newton_schulz, ctypes.byref(d), g.data_ptr(), out.data_ptr(),
           _addr(buf), 0 if buf is None else buf.numel(), stream=stream)
     return out
 
@@ -586,14 +588,14 @@ def muon_update(w, g, v, lr, momentum=0.95, weight_decay=0.0, nesterov=True, sca
     sqrt(max(1, rows / cols)).  `lr` is a number, or a one-element float32
     device tensor read when the kernel runs (for graph capture)."""
     _dev(w, "w", torch.float32)
-    dev = w.device
+    dev = w.get_device()
     _checked(dev, g, "g", torch.float32), _checked(dev, v, "v", torch.float32)
     if not (w.shape == g.shape == v.shape):
         raise ValueError("w, g and v must have the same shape")
     d = ns_desc(w.shape, steps, coef, eps, group)
     if scale is None:
         scale = max(1.0, d.rows / max(1, d.cols)) ** 0.5
-    buf = (ws or Workspace(dev)).get(newton_schulz_workspace_size(d))
+    buf = (ws or Workspace(w.device)).get(newton_schulz_workspace_size(d))
     _checked(dev, buf, "workspace", torch.uint8)
     on_device = isinstance(lr, torch.Tensor)
     if on_device:
@@ -629,22 +631,23 @@ def quantize_rows(x, q=None, scale=None, stream=None):
     """x (rows, ...) float32 or bfloat16, e.g. an inner product's weight or its
     bottom -> (q, scale): int8 rows padded with zeros to int8_pitch(cols)
     bytes, and float32 scales, with x[r] near q[r, :cols] * scale[r]."""
-    if x.dtype not in _ROW_TYPES:
+    kind = _ROW_TYPES.get(x.dtype)
+    if kind is None:
         raise ValueError(f"x must be float32 or bfloat16, got {x.dtype}")
-    _dev(x, "x", x.dtype)
+    _dev(x, "x")
     if x.dim() < 2:
         raise ValueError("x must have rows and columns")
-    dev, rows, cols = x.device, x.shape[0], _row_values(x)
+    dev, rows, cols = x.get_device(), x.shape[0], _row_values(x)
     pitch = int8_pitch(cols)
     if q is None:
-        q = torch.empty((rows, pitch), dtype=torch.int8, device=dev)
+        q = x.new_empty((rows, pitch), dtype=torch.int8)
     if scale is None:
-        scale = torch.empty(rows, dtype=torch.float32, device=dev)
+        scale = x.new_empty(rows, dtype=torch.float32)
     _checked(dev, q, "q", torch.int8), _checked(dev, scale, "scale", torch.float32)
     if q.shape != (rows, pitch) or scale.numel() != rows:
         raise ValueError(f"q must be {(rows, pitch)} and scale {(rows,)}")
-    _call(dev, load().caffe_quantize_rows, x.data_ptr(), _ROW_TYPES[x.dtype], rows, cols,
-          q.data_ptr(), scale.data_ptr(), stream=stream)
+    _call(dev, load().caffe_quantize_rows, x.data_ptr(), kind, rows, cols, q.data_ptr(),
+          scale.data_ptr(), stream=stream)
     return q, scale
 
 
@@ -654,16 +657,19 @@ def inner_product_int8(x, weight, weight_scale, bias=None, C=None, x_scale=None,
     quantize_rows makes them; x (N, ...) of C values a sample in float32 or
     bfloat16 (brought to 8-bit rows in the call), or int8 rows with x_scale.
     C (the values of a row) may be left out for a float x."""
-    rows8 = x.dtype == torch.int8
-    if not rows8 and x.dtype not in _ROW_TYPES:
+    kind = CAFFE_INT8_ROWS if x.dtype is torch.int8 else _ROW_TYPES.get(x.dtype)
+    if kind is None:
         raise ValueError(f"bottom must be float32, bfloat16 or int8, got {x.dtype}")
-    if top_dtype not in _ROW_TYPES:
+    top_kind = _ROW_TYPES.get(top_dtype)
+    if top_kind is None:
         raise ValueError(f"top must be float32 or bfloat16, got {top_dtype}")
-    _dev(x, "bottom", x.dtype)
-    dev = x.device
+    rows8 = kind == CAFFE_INT8_ROWS
+    _dev(x, "bottom")
+    dev = x.get_device()
     _checked(dev, weight, "weight", torch.int8)
-    for t, name in ((weight_scale, "weight_scale"), (bias, "bias"), (x_scale, "bottom_scale")):
-        _checked(dev, t, name, torch.float32)
+    _checked(dev, weight_scale, "weight_scale", torch.float32)
+    _checked(dev, bias, "bias", torch.float32)
+    _checked(dev, x_scale, "bottom_scale", torch.float32)
     if x.dim() < 2 or weight.dim() != 2:
         raise ValueError("bottom must have rows, weight (K, pitch)")
     N, per = x.shape[0], _row_values(x)
@@ -671,8 +677,8 @@ def inner_product_int8(x, weight, weight_scale, bias=None, C=None, x_scale=None,
         if rows8:
             raise ValueError("8-bit rows need C, the values of a row")
         C = per
-    pitch, K = int8_pitch(C), weight.shape[0]
-    if weight.shape[1] != pitch or per != (pitch if rows8 else C):
+    pitch, (K, w_pitch) = int8_pitch(C), weight.shape
+    if w_pitch != pitch or per != (pitch if rows8 else C):
         raise ValueError(f"rows of C={C} values take {pitch} bytes: weight {tuple(weight.shape)}, "
                          f"bottom {tuple(x.shape)}")
     if rows8 != (x_scale is not None) or (rows8 and x_scale.numel() != N):
@@ -680,20 +686,21 @@ def inner_product_int8(x, weight, weight_scale, bias=None, C=None, x_scale=None,
     if weight_scale.numel() != K or (bias is not None and bias.numel() != K):
         raise ValueError(f"weight_scale and bias must have K={K} elements")
     if out is None:
-        out = torch.empty((N, K), dtype=top_dtype, device=dev)
-    _checked(dev, out, "top", top_dtype)
-    if out.numel() != N * K:
-        raise ValueError(f"top must have {N} x {K} elements")
-    d = Ip8Desc(N, int(C), K, int(bool(relu)), CAFFE_INT8_ROWS if rows8 else _ROW_TYPES[x.dtype],
-                _ROW_TYPES[top_dtype])
-    lib = load()
-    desc, buf = ctypes.byref(d), None
+        out = x.new_empty((N, K), dtype=top_dtype)
+    else:
+        _checked(dev, out, "top", top_dtype)
+        if out.numel() != N * K:
+            raise ValueError(f"top must have {N} x {K} elements")
+    desc = ctypes.byref(Ip8Desc(N, int(C), K, 1 if relu else 0, kind, top_kind))
+    lib, buf, buf_bytes = load(), None, 0
     if not rows8:
         n = ctypes.c_size_t()
         check(lib.caffe_inner_product_int8_workspace_size(desc, ctypes.byref(n)))
-        buf = (ws or Workspace(dev)).get(n.value)
-        _checked(dev, buf, "workspace", torch.uint8)
+        buf = (ws or Workspace(x.device)).get(n.value)
+        if buf is not None:
+            _checked(dev, buf, "workspace", torch.uint8)
+            buf, buf_bytes = buf.data_ptr(), buf.numel()
     _call(dev, lib.caffe_inner_product_int8, desc, x.data_ptr(), _addr(x_scale),
-          weight.data_ptr(), weight_scale.data_ptr(), _addr(bias), out.data_ptr(), _addr(buf),
-          0 if buf is None else buf.numel(), stream=stream)
+          weight.data_ptr(), weight_scale.data_ptr(), _addr(bias), out.data_ptr(), buf, buf_bytes,
+          stream=stream)
     return out
