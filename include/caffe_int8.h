@@ -63,7 +63,8 @@ int caffe_quantize_rows(const void* x, int32_t dtype, int64_t rows, int32_t cols
 /* Host-only: bytes of device workspace of caffe_inner_product_int8. */
 int caffe_inner_product_int8_workspace_size(const caffe_ip8_desc* desc, size_t* bytes);
 
-/* bottom: N x C values, or with CAFFE_INT8_ROWS N 8-bit rows and bottom_scale
+/* N and K are at most 2^26, N x K at most 2^23 tiles of 64 x 64 (else
+ * CAFFE_ERR_UNSUPPORTED).  bottom: N x C values, or with CAFFE_INT8_ROWS N 8-bit rows and bottom_scale
  * (N floats; NULL otherwise).  weight: K 8-bit rows with weight_scale (K
  * floats).  bias: K floats or NULL. */
 int caffe_inner_product_int8(const caffe_ip8_desc* desc, const void* bottom,

@@ -2942,8 +2942,11 @@ static int check_ip8(const caffe_ip8_desc* d)
         return fail(CAFFE_ERR_UNSUPPORTED, "unknown top type %d", d->top_type);
     if (caffe_int8_pitch(d->C) == 0)
         return fail(CAFFE_ERR_UNSUPPORTED, "C must be <= 2^17 (exact 32-bit sums)");
-    if (d->N > (1 << 30) || d->K > (1 << 30) || ((int64_t)d->N / 64 + 1) * (d->K / 64 + 1) > (1 << 30))
-        return fail(CAFFE_ERR_UNSUPPORTED, "N x K has more than 2^30 tiles of 64 x 64");
+    // (a launch holds fewer than 2^32 threads)
+    if (d->N > (1 << 26) || d->K > (1 << 26) ||
+        ((int64_t)d->N / 64 + 1) * (d->K / 64 + 1) > (1 << 23))
+        return fail(CAFFE_ERR_UNSUPPORTED,
+                    "N and K must be <= 2^26, and N x K at most 2^23 tiles of 64 x 64");
     return CAFFE_OK;
 }
 

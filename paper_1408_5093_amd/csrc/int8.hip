@@ -382,20 +382,29 @@ hipError_t launch_ip8_quant(const Ip8Params& p, const void* x, int C, hipStream_
 hipError_t launch_quantize_rows(const void* x, int bf16, int64_t rows, int cols, int pitch,
                                 int8_t* q, float* scale, hipStream_t s)
 {
-    if (rows == 0)
-        return hipSuccess;
-    if (bf16) {
-        if (cols % 4 == 0)
-            quantize_rows<uint16_t, 4>((const uint16_t*)x, rows, cols, pitch, q, scale, s);
-        else
-            quantize_rows<uint16_t, 1>((const uint16_t*)x, rows, cols, pitch, q, scale, s);
-    } else {
-        if (cols % 4 == 0)
-            quantize_rows<float, 4>((const float*)x, rows, cols, pitch, q, scale, s);
-        else
-            quantize_rows<float, 1>((const float*)x, rows, cols, pitch, q, scale, s);
+    // a launch holds fewer than 2^32 threads: 2^21 rows at a time
+    constexpr int64_t kRows = 1 << 21;
+    for (int64_t r = 0; r < rows; r += kRows) {
+        const int64_t n = std::min(kRows, rows - r);
+        int8_t* to = q + r * pitch;
+        if (bf16) {
+            const uint16_t* p = (const uint16_t*)x + r * cols;
+            if (cols % 4 == 0)
+                quantize_rows<uint16_t, 4>(p, n, cols, pitch, to, scale + r, s);
+            else
+                quantize_rows<uint16_t, 1>(p, n, cols, pitch, to, scale + r, s);
+        } else {
+            const float* p = (const float*)x + r * cols;
+            if (cols % 4 == 0)
+                quantize_rows<float, 4>(p, n, cols, pitch, to, scale + r, s);
+            else
+                quantize_rows<float, 1>(p, n, cols, pitch, to, scale + r, s);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 hipError_t launch_inner_product_int8(const Ip8Args& a, char* ws, hipStream_t s)

@@ -144,6 +144,7 @@ def _ip8(**kw):
     ("N", -1, INVALID), ("C", 0, INVALID), ("K", 0, INVALID), ("relu", 2, INVALID),
     ("bottom_type", 2, UNSUPPORTED), ("top_type", 16, UNSUPPORTED),
     ("C", (1 << 17) + 1, UNSUPPORTED), ("N", 1 << 30, UNSUPPORTED),
+    ("N", (1 << 26) + 1, UNSUPPORTED), ("K", (1 << 26) + 1, UNSUPPORTED), ("N", 1 << 16, UNSUPPORTED),
 ])
 def test_inner_product_int8_descriptor(field, value, code):
     lib = cc.load()

@@ -111,6 +111,18 @@ def test_quantize_rows_past_2_31_bytes():
     assert int(torch.count_nonzero(y[:-3])) == 0
 
 
+def test_quantize_more_rows_than_a_launch_takes():
+    """Rows past 2^21, where the next launch begins, on both sides of it."""
+    rows, cols = (1 << 21) + 70, 5
+    print("quantize (2^21 + 70) x 5", flush=True)
+    x = torch.zeros((rows, cols), device=DEV)
+    mid = np.random.default_rng(27).standard_normal((90, cols)).astype(np.float32)
+    x[(1 << 21) - 20:] = dev(mid)
+    q, s = cc.quantize_rows(x)
+    check_rows(q[-90:], s[-90:], mid)
+    assert int(torch.count_nonzero(s)) == 90 and int(torch.count_nonzero(q[:-90])) == 0
+
+
 def ip_ref(q, s, p, t, bias, relu):
     """(top, the sum of its terms' sizes)."""
     z = (q.astype(np.int64) @ p.astype(np.int64).T).astype(np.float64)
@@ -157,6 +169,26 @@ def test_inner_product(N, C, K, bottom, top, relu, bias):
         y = cc.inner_product_int8(xt, wq, wsc, bt, relu=relu, top_dtype=top)
     assert y.dtype == top
     check_top(y, *ip_ref(q, s, p, t, b, relu))
+
+
+@pytest.mark.parametrize("N,C,K", [(2000, 2000, 4001), (1990, 2050, 4000), (4000, 4096, 4093),
+                                   (8200, 1000, 8192)])
+@pytest.mark.parametrize("top", [torch.float32, torch.bfloat16])
+def test_inner_product_large(N, C, K, top):
+    """Sizes that take tiles of 128 and 256, against whole numbers in the device's
+    double precision (sums below 2^53)."""
+    print(f"int8 product N={N} C={C} K={K} {top}", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(N + C + K)
+    w, ws = cc.quantize_rows(torch.randn((K, C), generator=gen, device=DEV))
+    x, xs = cc.quantize_rows(torch.randn((N, C), generator=gen, device=DEV).clamp_(min=0))
+    b = torch.randn(K, generator=gen, device=DEV)
+    y = cc.inner_product_int8(x, w, ws, b, C=C, x_scale=xs, top_dtype=top)
+    z = (x.double() @ w.double().t().contiguous()) * xs.double()[:, None] * ws.double()
+    ref = z + b.double()
+    tol = TOL * (z.abs() + b.double().abs())
+    if top == torch.bfloat16:
+        tol += TOL_BF16 * ref.abs()
+    assert bool(((y.double() - ref).abs() <= tol).all())
 
 
 @pytest.mark.parametrize("N", [1, 6, 40, 200])

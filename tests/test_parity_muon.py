@@ -169,6 +169,66 @@ def test_newton_schulz_in_place_any_workspace_any_stream(rows, cols):
     assert torch.equal(out, first)
 
 
+def ns_ref_gpu(g, steps):
+    """ns_ref of one matrix with the device's double-precision products."""
+    a, b, c = (float(np.float32(v)) for v in cc.NS_COEF)
+    x = g.double()
+    tall = x.shape[0] > x.shape[1]
+    x = x.t().contiguous() if tall else x
+    x = x / (torch.linalg.vector_norm(x) + float(np.float32(1e-7)))
+    for _ in range(steps):
+        A = x @ x.t().contiguous()
+        x = a * x + (b * A + c * (A @ A)) @ x
+    return x.t() if tall else x
+
+
+# sizes from which the products take tiles of 128, 192 and 256 x 192, round and
+# odd, tall and wide
+LARGE = [(2600, 2601), (3400, 3300), (1500, 7001), (4090, 4100), (4097, 3900), (4080, 9101),
+         (9100, 4080)]
+
+
+@pytest.mark.parametrize("rows,cols", LARGE)
+def test_newton_schulz_large(rows, cols):
+    print(f"newton_schulz {rows}x{cols}", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(rows + cols)
+    d = torch.randn((rows, 64), generator=gen, device=DEV)
+    x = torch.randn((64, cols), generator=gen, device=DEV)
+    g = (d @ x / 64 + 0.2 * torch.randn((rows, cols), generator=gen, device=DEV)) * 1e-3
+    o = cc.newton_schulz(g)
+    ref = ns_ref_gpu(g, 5)
+    norm = torch.linalg.vector_norm(ref)
+    assert float(torch.linalg.vector_norm(o.double() - ref) / norm) <= TOL
+    # the update along it, from a zero history: u = (1 + momentum) g
+    w = torch.randn((rows, cols), generator=gen, device=DEV) * 0.01
+    w0, v = w.double(), torch.zeros_like(g)
+    cc.muon_update(w, g, v, 0.5, weight_decay=0.1, scale=0.3)
+    assert torch.equal(v, g)
+    want = w0 - 0.5 * (float(np.float32(0.3)) * ref + float(np.float32(0.1)) * w0)
+    err = float(torch.linalg.vector_norm(w.double() - want))
+    # eps counts against 1.95 times the norm here: 1e-7 / ||g|| more, ||g|| > 0.1
+    step = 0.15 * float(norm)
+    assert err <= (TOL + 1e-6) * step + 2.0 ** -22 * (float(torch.linalg.vector_norm(w0)) + step)
+    ob = cc.newton_schulz(g.bfloat16())
+    rb = ns_ref_gpu(g.bfloat16(), 5)
+    assert float(torch.linalg.vector_norm(ob.double() - rb) / norm) <= TOL_BF16
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(3000, 4, 4), (300, 33, 20), (200, 20, 700),
+                                             (40, 129, 130)])
+def test_newton_schulz_many_matrices(batch, rows, cols):
+    print(f"newton_schulz {batch} x {rows}x{cols}", flush=True)
+    g = gradient(np.random.default_rng([11, rows]), batch, rows, cols)
+    out = cc.newton_schulz(dev(g))
+    pick = [0, 1, batch // 2, batch - 1]
+    ref = ns_ref(g[pick], 5)
+    # (four by four: singular values may vanish in few dimensions)
+    assert rel(out[pick], ref) <= (HARD if rows == 4 else TOL)
+    assert torch.isfinite(out).all()
+    one = cc.newton_schulz(dev(g[batch - 1]))
+    assert torch.equal(out[batch - 1], one)
+
+
 def muon_ref(w, g, v, lr, mu, wd, nesterov, scale, steps=5):
     f = lambda t: float(np.float32(t))  # noqa: E731
     w, g, v = (np.asarray(t, dtype=np.float64) for t in (w, g, v))
