@@ -191,7 +191,9 @@ __device__ __forceinline__ float ip8_finish(int acc, float s, float t, float bia
     return z > 0.f ? z : (relu ? 0.f : z);
 }
 
-// 64 x 64 and 128 x 128 by four waves, 256 x 256 by eight
+// 32 x 32 by four waves that share the reduction, 64 x 64 and 128 x 128 by 2 x 2
+// waves, 256 x 256 by eight
+typedef TileShared<OpInt8Line, 4, false> Ip8Tile32;
 typedef TileNT<OpInt8Line, 2, 2, 1, 1, 5, false> Ip8Tile64;
 typedef TileNT<OpInt8Line, 2, 2, 2, 2, 2, false> Ip8Tile128;
 typedef TileNT<OpInt8Half, 4, 2, 2, 4, 2, false> Ip8Tile256;
@@ -257,124 +259,106 @@ hipError_t launch_ip8_tile(const Ip8Params& p, hipStream_t s)
     return hipGetLastError();
 }
 
-// A few samples: the stream of the weights.  A workgroup takes 16 outputs, its
+// One float sample: the stream of the weights.  A workgroup takes 16 outputs, its
 // eight waves a share of the reduction each, 64 bytes of every weight row to a
 // step of the 16x16x64 instruction straight from memory (lane l: row l % 16,
-// bytes 16 (l / 16) ..), and the shares are added in LDS.  QUANT (one sample of at most kQuantRow values): the workgroup
-// brings the float sample to 8 bits itself, while its first weights are on
-// their way; otherwise 8-bit rows are read as the weights are.
-constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves;
-constexpr int kQuantRow = 16384;
-constexpr int kFewSamples = 16;  // (a tile of 64 is as fast at 20: 4096 x 9216 15.6 / 15.9 us)
+// bytes 16 (l / 16) ..), and the shares are added in LDS.  The workgroup brings
+// the sample to 8 bits itself while its first weights are on their way: 4096 x
+// 9216 takes 11.4 us, a launch for the rounding and a tiled product 4.3 + 9.3.
+constexpr int kOneWaves = 8, kOneThreads = 64 * kOneWaves;
+constexpr int kOneRow = 16384;  // values of the sample, at most
 
-template <typename T, int VEC, bool QUANT>
-__global__ void __launch_bounds__(kFewThreads)
-ip8_few_kernel(const Ip8Params p, const T* __restrict__ xf, int C)
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kOneThreads)
+ip8_one_kernel(const Ip8Params p, const T* __restrict__ x, int C)
 {
     constexpr int U = 8;  // steps in flight
-    __shared__ u32x4 xq[QUANT ? kQuantRow / 16 : 1];
-    __shared__ uint32_t top[kFewWaves];
-    float xscale = 0.f;
-    __shared__ int sum[kFewWaves][256];
+    __shared__ u32x4 xq[kOneRow / 16];
+    __shared__ uint32_t top[kOneWaves];
+    __shared__ int sum[kOneWaves][16];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int k0 = blockIdx.x * 16;
     const int steps = (int)(p.pitch / 64);
-    const int t0 = steps * wave / kFewWaves, t1 = steps * (wave + 1) / kFewWaves;
+    const int t0 = steps * wave / kOneWaves, t1 = steps * (wave + 1) / kOneWaves;
     // rows past the last re-read it: their results are not stored
     const int8_t* w = p.w + (size_t)min(k0 + r, p.K - 1) * p.pitch + g * 16;
-    const int8_t* x = p.x + (size_t)min(r, p.N - 1) * p.pitch + g * 16;
-    intx4 acc = {0, 0, 0, 0};
-    intx4 wv[U], xv[U];
+    intx4 acc = {0, 0, 0, 0}, wv[U];
     auto load = [&](int t) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int c = min(t + u, steps - 1) * 64;
-            wv[u] = *(const intx4*)(w + c);
-            if constexpr (!QUANT)
-                xv[u] = *(const intx4*)(x + c);
-        }
+        for (int u = 0; u < U; ++u)
+            wv[u] = *(const intx4*)(w + min(t + u, steps - 1) * 64);
     };
     load(t0);
-    if constexpr (QUANT) {
-        constexpr int CH = kQuantRow / (kFewThreads * 4);
-        float y[CH][4];
-        uint32_t m = 0;
+    constexpr int CH = kOneRow / (kOneThreads * 4);
+    float y[CH][4];
+    uint32_t m = 0;
 #pragma unroll
-        for (int h = 0; h < CH; ++h) {
-            const int c = (h * kFewThreads + (int)threadIdx.x) * 4;
-            load4<T, VEC>(xf + c, C - c, y[h]);
+    for (int h = 0; h < CH; ++h) {
+        const int c = (h * kOneThreads + (int)threadIdx.x) * 4;
+        load4<T, VEC>(x + c, C - c, y[h]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                m = max(m, __builtin_bit_cast(uint32_t, y[h][e]) & 0x7FFFFFFFu);
-        }
-        for (int off = 32; off > 0; off >>= 1)
-            m = max(m, (uint32_t)__shfl_xor((int)m, off, 64));
-        if (lane == 0)
-            top[wave] = m;
-        __syncthreads();
-#pragma unroll
-        for (int v = 0; v < kFewWaves; ++v)
-            m = max(m, top[v]);
-        xscale = row_scale(m);
-#pragma unroll
-        for (int h = 0; h < CH; ++h) {
-            const int c = (h * kFewThreads + (int)threadIdx.x) * 4;
-            if (c < (int)p.pitch)
-                ((uint32_t*)xq)[c / 4] = round_row4(y[h], xscale);
-        }
-        __syncthreads();
+        for (int e = 0; e < 4; ++e)
+            m = max(m, __builtin_bit_cast(uint32_t, y[h][e]) & 0x7FFFFFFFu);
     }
+    for (int off = 32; off > 0; off >>= 1)
+        m = max(m, (uint32_t)__shfl_xor((int)m, off, 64));
+    if (lane == 0)
+        top[wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < kOneWaves; ++v)
+        m = max(m, top[v]);
+    const float xscale = row_scale(m);
+#pragma unroll
+    for (int h = 0; h < CH; ++h) {
+        const int c = (h * kOneThreads + (int)threadIdx.x) * 4;
+        if (c < (int)p.pitch)
+            ((uint32_t*)xq)[c / 4] = round_row4(y[h], xscale);
+    }
+    __syncthreads();
     for (int t = t0; t < t1; t += U) {
         if (t > t0)
             load(t);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if constexpr (QUANT) {
-                xv[u] = intx4{0, 0, 0, 0};
-                if (r == 0 && t + u < t1)
-                    xv[u] = __builtin_bit_cast(intx4, xq[(t + u) * 4 + g]);
-            }
-            if (t + u < t1)
-                acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(xv[u], wv[u], acc, 0, 0, 0);
+            if (t + u >= t1)
+                break;
+            intx4 xv = {0, 0, 0, 0};
+            if (r == 0)
+                xv = __builtin_bit_cast(intx4, xq[(t + u) * 4 + g]);
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(xv, wv[u], acc, 0, 0, 0);
         }
     }
-    // lane l holds samples 4 g + q of output l % 16
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-        sum[wave][(4 * g + q) * 16 + r] = acc[q];
+    if (g == 0)  // lane l < 16 holds the sample and output l
+        sum[wave][r] = acc[0];
     __syncthreads();
-    const int i = threadIdx.x, n = i >> 4, k = k0 + (i & 15);
-    if (n < p.N && k < p.K) {
+    const int k = k0 + (int)threadIdx.x;
+    if (threadIdx.x < 16 && k < p.K) {
         int s = 0;
 #pragma unroll
-        for (int v = 0; v < kFewWaves; ++v)
-            s += sum[v][i];
-        const float z = ip8_finish(s, QUANT ? xscale : p.xs[n], p.ws[k],
-                                   p.bias ? p.bias[k] : 0.f, p.relu);
-        const size_t at = (size_t)n * p.K + k;
+        for (int v = 0; v < kOneWaves; ++v)
+            s += sum[v][threadIdx.x];
+        const float z = ip8_finish(s, xscale, p.ws[k], p.bias ? p.bias[k] : 0.f, p.relu);
         if (p.out_bf16)
-            p.out_bf16[at] = f32_to_bf16_rne(z);
+            p.out_bf16[k] = f32_to_bf16_rne(z);
         else
-            p.out_f32[at] = z;
+            p.out_f32[k] = z;
     }
-}
-
-template <typename T, int VEC, bool QUANT>
-hipError_t launch_ip8_few(const Ip8Params& p, const void* x, int C, hipStream_t s)
-{
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ip8_few_kernel<T, VEC, QUANT>),
-                       dim3((unsigned)((p.K + 15) / 16)), dim3(kFewThreads), 0, s, p,
-                       (const T*)x, C);
-    return hipGetLastError();
 }
 
 template <typename T>
-hipError_t launch_ip8_quant(const Ip8Params& p, const void* x, int C, hipStream_t s)
+hipError_t launch_ip8_one(const Ip8Params& p, const void* x, int C, hipStream_t s)
 {
-    return C % 4 == 0 ? launch_ip8_few<T, 4, true>(p, x, C, s)
-                      : launch_ip8_few<T, 1, true>(p, x, C, s);
+    const dim3 grid((unsigned)((p.K + 15) / 16)), threads(kOneThreads);
+    if (C % 4 == 0)
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(ip8_one_kernel<T, 4>), grid, threads, 0, s, p,
+                           (const T*)x, C);
+    else
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(ip8_one_kernel<T, 1>), grid, threads, 0, s, p,
+                           (const T*)x, C);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -421,9 +405,9 @@ hipError_t launch_inner_product_int8(const Ip8Args& a, char* ws, hipStream_t s)
     p.K = a.K;
     p.relu = a.relu;
     p.pitch = (uint32_t)a.pitch;
-    if (a.bottom_type != kIp8BottomInt8 && a.N == 1 && a.pitch <= kQuantRow)
-        return a.bottom_type == kIp8BottomBf16 ? launch_ip8_quant<uint16_t>(p, a.bottom, a.C, s)
-                                               : launch_ip8_quant<float>(p, a.bottom, a.C, s);
+    if (a.bottom_type != kIp8BottomInt8 && a.N == 1 && a.pitch <= kOneRow)
+        return a.bottom_type == kIp8BottomBf16 ? launch_ip8_one<uint16_t>(p, a.bottom, a.C, s)
+                                               : launch_ip8_one<float>(p, a.bottom, a.C, s);
     if (a.bottom_type == kIp8BottomInt8) {
         p.x = (const int8_t*)a.bottom;
         p.xs = a.bottom_scale;
@@ -437,26 +421,25 @@ hipError_t launch_inner_product_int8(const Ip8Args& a, char* ws, hipStream_t s)
         p.x = q;
         p.xs = qs;
     }
-    if (a.N <= kFewSamples)
-        return launch_ip8_few<float, 1, false>(p, nullptr, a.C, s);
-    // The tile by a model of the time on 256 compute units, us: a launch and its
-    // epilogue, and per line of 128 values `one` while every unit has at most
-    // one tile, else `each` for each tile of the fullest.  Measured / modelled:
-    //        64 x 4096 x 4096  1024 x 4096 x 4096  4096 x 4096 x 4096  8192 x 9216 x 4096
-    //   64        11 / 11            35 / 34             129 / 123          521 / 535
-    //   128       30 / 34            35 / 34              94 / 89           342 / 358
-    //   256       57 / 84            65 / 84              86 / 84           298 / 297
-    auto cost = [&](int64_t tm, int64_t tn, double over, double one, double each) {
-        const int64_t n = ((a.N + tm - 1) / tm * ((a.K + tn - 1) / tn) + 255) / 256;
-        return over + a.pitch / 128 * (n <= 1 ? one : each * (double)n);
-    };
-    const double c64 = cost(64, 64, 5.0, 0.19, 0.23);
-    const double c128 = cost(128, 128, 12.0, 0.70, 0.60);
-    const double c256 = cost(256, 256, 23.0, 1.90, 1.90);
-    if (c256 < c128 && c256 < c64)
+    // The tile by the model of its time.  Measured / modelled, us:
+    //        20 x 9216 x 4096  64 x 4096 x 4096  1024 x 4096 x 4096  4096 x 4096 x 4096  8192 x 9216 x 4096
+    //   32        10 / 11          7.4 / 7.1
+    //   64        15 / 19           11 / 11            35 / 34             129 / 123          521 / 535
+    //   128                         30 / 34            35 / 34              94 / 89           342 / 358
+    //   256                         57 / 84            65 / 84              86 / 84           298 / 297
+    auto tiles = [&](int64_t side) { return (a.N + side - 1) / side * ((a.K + side - 1) / side); };
+    const int64_t lines = a.pitch / 128;
+    const double t32 = TileTime{3.9, 0.10, 0.18}.of(tiles(32), lines);
+    const double t64 = TileTime{5.0, 0.19, 0.23}.of(tiles(64), lines);
+    const double t128 = TileTime{12.0, 0.70, 0.60}.of(tiles(128), lines);
+    const double t256 = TileTime{23.0, 1.90, 1.90}.of(tiles(256), lines);
+    const double least = std::min(std::min(t32, t64), std::min(t128, t256));
+    if (t256 <= least)
         return launch_ip8_tile<Ip8Tile256>(p, s);
-    if (c128 < c64)
+    if (t128 <= least)
         return launch_ip8_tile<Ip8Tile128>(p, s);
+    if (t32 < t64)
+        return launch_ip8_tile<Ip8Tile32>(p, s);
     return launch_ip8_tile<Ip8Tile64>(p, s);
 }
 

@@ -545,6 +545,19 @@ hipError_t launch_softmax_loss(const float* z, const int32_t* labels, int N, int
 hipError_t launch_sgd_update(float* w, const float* g, float* v, int64_t count, float lr,
                              const float* lr_dev, float momentum, float decay, hipStream_t s);
 
+// ---- tile products (tile_gemm.h)
+// The time of a product by its tiles, us: `over` for the launch and its
+// epilogue, and per line of the reduction `one` while each of the 256 compute
+// units has at most one tile, else `each` for every tile of the fullest.
+struct TileTime {
+    double over, one, each;
+    double of(int64_t tiles, int64_t lines) const
+    {
+        const int64_t n = (tiles + 255) / 256;
+        return over + (double)lines * (n <= 1 ? one : each * (double)n);
+    }
+};
+
 // ---- orthogonalised updates (muon.hip)
 constexpr int kNsMaxSteps = 64;
 constexpr double kNsMaxRange = 1024.0;  // of the iteration's singular values squared, and of q

@@ -205,10 +205,11 @@ __device__ __forceinline__ void tile_at(int t, int mt, int nt, int& I, int& J)
     }
 }
 
-// 64 x 64 and 128 x 128 by four waves, with accumulators for the low terms;
-// 192 x 192 by four waves and 256 x 192 by eight, whose accumulators fill the
+// 32 x 32 by four waves that share the reduction, 64 x 64 and 128 x 128 by 2 x 2
+// waves, all with accumulators for the low terms; 192 x 192 by four waves and 256 x 192 by eight, whose accumulators fill the
 // registers.
 typedef TileNT<OpPairLine, 2, 2, 1, 1, 5, true> Tile64;
+typedef TileShared<OpPairLine, 4, true> Tile32;
 typedef TileNT<OpPair, 2, 2, 2, 2, 2, true> Tile128;
 typedef TileNT<OpPair, 2, 2, 3, 3, 3, false> Tile192;
 typedef TileNT<OpPair, 4, 2, 2, 3, 2, false> Tile256;
@@ -248,13 +249,8 @@ ns_gemm_kernel(const NsGemm p)
         pre[2 * q] = *(const u32x2*)r;
         pre[2 * q + 1] = *(const u32x2*)(r + 64);
     };
-    if constexpr (PRE) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            load_r(q, m0 + (wave & 1) * 32 + 4 * (lane >> 5) + 8 * q,
-                   n0 + (wave >> 1) * 32 + (lane & 31));
-    }
+    if constexpr (PRE)
+        Tile::positions([&](int q, int di, int dj) { load_r(q, m0 + di, n0 + dj); });
     typename Tile::acc_t acc[Tile::kMI][Tile::kNI];
     Tile::run(A, (uint32_t)min(Tile::TM, p.M - m0) * p.a_pitch, p.a_pitch, B,
               (uint32_t)min(Tile::TN, p.N - n0) * p.b_pitch, p.b_pitch, s0, s1 - s0, acc);
@@ -466,36 +462,39 @@ hipError_t launch_tile(const NsGemm& p, hipStream_t s)
     return hipGetLastError();
 }
 
-// The tile by a model of the time on 256 compute units: `over` us for a launch
-// and its epilogue, and per stage of 32 reduction elements `one` us while every
-// unit has at most one tile, else `each` us for each tile of the fullest unit.
-// Fitted to 200 x 200 .. 4096 x 9216; us measured / modelled, symmetric
-// products m = 512 .. 4096 and 4096 x 9216 x 4096:
-//          512       1280      1800      2560      3000       4096       x 9216
-//   64     8 / 8     15 / 15   33 / 34   93 / 90   129 / 130  255 / 315  1090 / 1250
-//   128    20 / 20   40 / 42   51 / 57   80 / 78   126 / 130  240 / 260  790 / 766
-//   192    33 / 33   56 / 64   73 / 86   101 / 116 125 / 134  185 / 178  900 / 844
-//   256 x 192 (full products only)                                       755 / 745
+// Fitted to 140 x 140 .. 4096 x 9216; us measured / modelled, symmetric products
+// of m = 200 .. 4096 and the full one of 4096 x 9216 x 4096:
+//          200       512       700       1280      1800      2560      3000       4096       x 9216
+//   32   5.1 / 5.3 6.5 / 6.5 8.0 / 7.4  30 / 30   63 / 68
+//   64   6.3 / 6.3 9.0 / 8.9  11 / 11   16 / 16   33 / 35   93 / 91   129 / 131  255 / 315  1090 / 1250
+//   128             20 / 20             40 / 42   51 / 57   80 / 78   126 / 130  240 / 260   790 / 766
+//   192             33 / 33             56 / 64   73 / 86  101 / 116  125 / 134  185 / 178   900 / 844
+//   256 x 192 (full products only)                                                           755 / 745
+constexpr TileTime kTime32 = {4.3, 0.14, 0.16}, kTime64 = {4.3, 0.29, 0.27},
+                   kTime128 = {6.0, 0.90, 0.66}, kTime192 = {12.0, 1.30, 1.30},
+                   kTime256 = {15.0, 1.90, 1.90};
+
+// The tile with the least time by the model.
 template <int EPI>
 hipError_t launch_gemm(const NsGemm& p, hipStream_t s)
 {
-    auto cost = [&](int64_t tiles, double over, double one, double each) {
-        const int64_t n = (tiles + 255) / 256;
-        return over + p.stages * (n <= 1 ? one : each * (double)n);
-    };
-    const double c64 = cost(tile_count<Tile64, EPI>(p), 3.5, 0.29, 0.27);
-    const double c128 = cost(tile_count<Tile128, EPI>(p), 6.0, 0.90, 0.66);
-    const double c192 = cost(tile_count<Tile192, EPI>(p), 12.0, 1.30, 1.30);
+    const double t32 = kTime32.of(tile_count<Tile32, EPI>(p), p.stages);
+    const double t64 = kTime64.of(tile_count<Tile64, EPI>(p), p.stages);
+    const double t128 = kTime128.of(tile_count<Tile128, EPI>(p), p.stages);
+    const double t192 = kTime192.of(tile_count<Tile192, EPI>(p), p.stages);
+    double least = std::min(std::min(t32, t64), std::min(t128, t192));
     if constexpr (EPI >= kEpiX) {
-        const double c256 = cost(tile_count<Tile256, EPI>(p), 15.0, 1.90, 1.90);
-        if (c256 < c64 && c256 < c128 && c256 < c192)
+        const double t256 = kTime256.of(tile_count<Tile256, EPI>(p), p.stages);
+        if (t256 < least)
             return launch_tile<Tile256, EPI>(p, s);
     }
-    if (c192 < c64 && c192 < c128)
+    if (t192 <= least)
         return launch_tile<Tile192, EPI>(p, s);
-    if (c128 < c64)
+    if (t128 <= least)
         return launch_tile<Tile128, EPI>(p, s);
-    return launch_tile<Tile64, EPI>(p, s);
+    if (t64 <= least)
+        return launch_tile<Tile64, EPI>(p, s);
+    return launch_tile<Tile32, EPI>(p, s);
 }
 
 }  // namespace
@@ -583,14 +582,22 @@ bool ns_plan(int batch, int rows, int cols, int steps, float a, float b, float c
     q->mm_bytes = ((size_t)q->m * mp + align) & ~align;
     q->xr_bytes = ((size_t)q->m * np + align) & ~align;
     q->xt_bytes = ((size_t)q->n * mp + align) & ~align;
-    const int64_t mt = (q->m + 63) / 64, tiles = mt * (mt + 1) / 2 * batch;
-    const int64_t stages = (int64_t)(np / 128);
-    // the Gram product of a short wide matrix has few tiles of long sums: its
-    // reduction is split until the tiles fill the 256 compute units, parts of
-    // at least four stages each
+    // The Gram product of a short wide matrix has few tiles of long sums.  Its
+    // reduction is split until tiles of 64 fill the 256 compute units, parts of
+    // at least four lines each, where that and the launch that adds the parts
+    // (3.5 us) take less time than the whole in one launch.
+    const int64_t lines = (int64_t)(np / 128);
+    auto tiles = [&](int64_t side) {
+        const int64_t t = (q->m + side - 1) / side;
+        return t * (t + 1) / 2 * batch;
+    };
     q->splits = 1;
-    if (batch > 0 && tiles < 128)
-        q->splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, stages / 4));
+    if (batch > 0) {
+        const int64_t s = std::min(256 / tiles(64), lines / 4);
+        if (s > 1 && kTime64.of(s * tiles(64), (lines + s - 1) / s) + 3.5 <
+                         std::min(kTime32.of(tiles(32), lines), kTime64.of(tiles(64), lines)))
+            q->splits = (int)s;
+    }
     q->norm_blocks = (int)std::min<int64_t>(kNormBlocks,
                                             ((int64_t)rows * cols + 4095) / 4096);
     size_t off = 0;

@@ -29,6 +29,7 @@ typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 // halves (2^-22 of it) left out.
 struct OpPair {
     typedef floatx16 acc_t;
+    typedef floatx4 acc4_t;
     static constexpr int kSteps = 2, kFrags = 2, kProds = 3;
     static constexpr int frag(int step, int f) { return step + 2 * f; }
     static constexpr int fa(int i) { return i == 2 ? 1 : 0; }
@@ -54,6 +55,7 @@ struct OpPairLine : OpPair {
 // 8-bit integers: a line is 128 reduction elements.
 struct OpInt8 {
     typedef intx16 acc_t;
+    typedef intx4 acc4_t;
     static constexpr int kSteps = 4, kFrags = 1, kProds = 1;
     static constexpr int frag(int step, int) { return step; }
     static constexpr int fa(int) { return 0; }
@@ -120,53 +122,65 @@ __device__ __forceinline__ void tile_wait_lds()
 
 // WM x WN waves of 32 MI x 32 NI each; LOW: products with a low term have
 // accumulators of their own (kProds > 1), so that they do not round the sum.
-template <class Op, int WM, int WN, int MI, int NI, int NS, bool LOW>
+// KW > 1: a wave forms the whole tile (WM = WN = 1) over every KW-th stage; its
+// sum is the caller's to add to the others' (TileShared).
+template <class Op, int WM, int WN, int MI, int NI, int NS, bool LOW, int KW = 1>
 struct TileNT {
     static constexpr int NW = WM * WN;
+    static_assert(KW == 1 || NW == 1, "one wave to a share of the reduction");
     static constexpr int TM = 32 * WM * MI, TN = 32 * WN * NI;
-    static constexpr int kThreads = 64 * NW;
+    static constexpr int kThreads = 64 * NW * KW;
     static constexpr int kMI = MI, kNI = NI;
-    static constexpr int kLdsBytes = (TM + TN) * 128 * NS;
+    static constexpr int kLdsBytes = (TM + TN) * 128 * NS * KW;
     // workgroups that one compute unit's LDS holds, and with them the waves on
     // each of its four SIMDs: the register budget
     static constexpr int kPerCu = 160 * 1024 / kLdsBytes > 4 ? 4 : 160 * 1024 / kLdsBytes;
-    static constexpr int kWavesPerSimd = kPerCu * NW / 4;
+    static constexpr int kWavesPerSimd = kPerCu * NW * KW / 4;
     typedef typename Op::acc_t acc_t;
 
-    // acc = A B^T over stages s0 .. s0 + nst - 1 (nst >= 1).  A points at the
+    // acc = A B^T over stages s0 .. s0 + all - 1 (all >= 1).  A points at the
     // tile's first row, a_bytes = rows in the tile * pitch (a row past it
     // reads as zeros), B likewise; TM * pitch < 2^31.
     static __device__ __forceinline__ void run(const void* A, uint32_t a_bytes, uint32_t a_pitch,
                                                const void* B, uint32_t b_bytes, uint32_t b_pitch,
-                                               int s0, int nst, acc_t (&acc)[MI][NI])
+                                               int s0, int all, acc_t (&acc)[MI][NI])
     {
         constexpr int NA = TM / 8 / NW, NB = TN / 8 / NW;  // copies per wave and stage
-        static_assert(TM % (8 * NW) == 0 && TN % (8 * NW) == 0 && NW % 2 == 0, "copy mapping");
+        static_assert(TM % (8 * NW) == 0 && TN % (8 * NW) == 0 && (NW == 1 || NW % 2 == 0),
+                      "copy mapping");
         // one array per buffer, A's rows then B's: the compiler tells the copies
         // to one from the reads of another by the array (it follows eight)
         static_assert(NS >= 2 && NS <= 8, "buffers");
         constexpr int kBuf = (TM + TN) * 8;
-        __shared__ u32x4 L0[kBuf], L1[kBuf], L2[NS > 2 ? kBuf : 1], L3[NS > 3 ? kBuf : 1];
-        __shared__ u32x4 L4[NS > 4 ? kBuf : 1], L5[NS > 5 ? kBuf : 1], L6[NS > 6 ? kBuf : 1];
-        __shared__ u32x4 L7[NS > 7 ? kBuf : 1];
-        u32x4* const Lb[8] = {L0, L1, L2, L3, L4, L5, L6, L7};
+        constexpr int kAll = kBuf * KW;
+        __shared__ u32x4 L0[kAll], L1[kAll], L2[NS > 2 ? kAll : 1], L3[NS > 3 ? kAll : 1];
+        __shared__ u32x4 L4[NS > 4 ? kAll : 1], L5[NS > 5 ? kAll : 1], L6[NS > 6 ? kAll : 1];
+        __shared__ u32x4 L7[NS > 7 ? kAll : 1];
 
-        const int tid = threadIdx.x;
-        const int lane = tid & 63;
-        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int lane = threadIdx.x & 63;
+        const int wave_id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int kw = KW > 1 ? wave_id : 0;  // this wave's share of the stages
+        const int wave = KW > 1 ? 0 : wave_id;
         const int wm = wave % WM, wn = wave / WM;
+        const int nst = KW > 1 ? (all - kw + KW - 1) / KW : all;
+        auto share = [&](u32x4* L, bool used) { return used ? L + kw * kBuf : L; };
+        u32x4* const Lb[8] = {share(L0, true),   share(L1, true),   share(L2, NS > 2),
+                              share(L3, NS > 3), share(L4, NS > 4), share(L5, NS > 5),
+                              share(L6, NS > 6), share(L7, NS > 7)};
 
         // copy i = wave + NW q moves tile rows 8 i .. 8 i + 7; of i, line_swz
-        // sees only bit 3 of the row, the wave's parity
+        // sees only bit 3 of the row, i's parity
         const int cr = lane >> 3;
-        const uint32_t ck = 16u * ((lane & 7) ^ line_swz(8 * wave + cr));
+        auto ck = [&](int q) {
+            return 16u * ((lane & 7) ^ line_swz(8 * (NW == 1 ? q : wave) + cr));
+        };
         uint32_t va[NA], vb[NB];
 #pragma unroll
         for (int q = 0; q < NA; ++q)
-            va[q] = (uint32_t)(8 * (wave + NW * q) + cr) * a_pitch + ck;
+            va[q] = (uint32_t)(8 * (wave + NW * q) + cr) * a_pitch + ck(q);
 #pragma unroll
         for (int q = 0; q < NB; ++q)
-            vb[q] = (uint32_t)(8 * (wave + NW * q) + cr) * b_pitch + ck;
+            vb[q] = (uint32_t)(8 * (wave + NW * q) + cr) * b_pitch + ck(q);
 #pragma unroll
         for (int q = 0; q < NA; ++q)
             va[q] = va[q] < a_bytes ? va[q] : kOob;
@@ -179,7 +193,7 @@ struct TileNT {
         // everywhere (a copy in a branch made the compiler wait for all of them)
         constexpr int NC = NA + NB;
         auto copy = [&](int t, u32x4* L, int c) {
-            const uint32_t soff = (uint32_t)(s0 + t) * 128u;
+            const uint32_t soff = (uint32_t)(s0 + t * KW + kw) * 128u;
             if (c < NA)
                 line_copy(make_rsrc(A, t < nst ? a_bytes : 0u), &L[(wave + NW * c) * 64], va[c],
                           soff);
@@ -259,10 +273,11 @@ struct TileNT {
                 if (t < P || CPS == NC || c < CPS)
                     copy(t, Lb[t], c);
         tile_wait<(NS - 2) * NC + CPS>();
-        tile_barrier();
+        if constexpr (NW > 1)
+            tile_barrier();
 #pragma unroll
         for (int r = 0; r < NR; ++r)
-            read(L0, 0, r, 0);
+            read(Lb[0], 0, r, 0);
         // whole turns of the buffers and of the two sets of fragments
         constexpr int U = NS * S % 2 ? 2 * NS : NS;
         for (int t0 = 0; t0 < nst; t0 += U) {
@@ -278,7 +293,8 @@ struct TileNT {
                              step + 1);
                 // stage t + 1 is there, stages t + 2 .. t + NS - 1 may be in flight
                 tile_wait_lds<(NS - 2) * NC>();
-                tile_barrier();
+                if constexpr (NW > 1)
+                    tile_barrier();
                 run_step((u * S + S - 1) & 1, 0, Lb[(h + 1) % NS], t + NS, Lb[h], 0);
             }
         }
@@ -328,6 +344,67 @@ struct TileNT {
     {
         each(acc, [](int, int, int) {},
              [&](int, int i, int j, auto& v) { f(i, j, v); });
+    }
+    // load(q, i, j) of a tile of one block to a wave, as each() calls it
+    template <class L>
+    static __device__ __forceinline__ void positions(L&& load)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            load(q, wave % WM * 32 + 4 * (lane >> 5) + 8 * q, wave / WM * 32 + (lane & 31));
+    }
+};
+
+// A 32 x 32 tile whose reduction four waves share, a fourth of the lines each
+// and no barriers between them; their sums are added in LDS in a fixed order,
+// each wave left with eight rows.  For products with few tiles: a compute unit
+// takes a line of a 64 x 64 tile's rows (16 KB) in 0.29 us or so, whatever the
+// number of buffers, the order of reads and copies or the instructions between
+// them, and four times as many units take a fourth each with half the bytes.
+template <class Op, int NS, bool LOW>
+struct TileShared {
+    typedef TileNT<Op, 1, 1, 1, 1, NS, LOW, 4> Share;
+    static constexpr int TM = 32, TN = 32, kThreads = 256, kMI = 1, kNI = 1;
+    static constexpr int kWavesPerSimd = 1;
+    typedef typename Op::acc4_t acc_t;
+
+    static __device__ __forceinline__ void run(const void* A, uint32_t a_bytes, uint32_t a_pitch,
+                                               const void* B, uint32_t b_bytes, uint32_t b_pitch,
+                                               int s0, int all, acc_t (&acc)[1][1])
+    {
+        __shared__ acc_t part[4][4][64];
+        typename Share::acc_t sum[1][1];
+        Share::run(A, a_bytes, a_pitch, B, b_bytes, b_pitch, s0, all, sum);
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            part[wave][q][lane] = acc_t{sum[0][0][4 * q], sum[0][0][4 * q + 1],
+                                        sum[0][0][4 * q + 2], sum[0][0][4 * q + 3]};
+        __syncthreads();
+        acc[0][0] = (part[0][wave][lane] + part[1][wave][lane]) +
+                    (part[2][wave][lane] + part[3][wave][lane]);
+    }
+    template <class L>
+    static __device__ __forceinline__ void positions(L&& load)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        load(0, 8 * wave + 4 * (lane >> 5), lane & 31);
+    }
+    template <class L, class F>
+    static __device__ __forceinline__ void each(const acc_t (&acc)[1][1], L&& load, F&& use)
+    {
+        positions(load);
+        positions([&](int q, int i, int j) {
+            decltype(acc[0][0][0] + acc[0][0][0]) v[4] = {acc[0][0][0], acc[0][0][1],
+                                                          acc[0][0][2], acc[0][0][3]};
+            use(q, i, j, v);
+        });
+    }
+    template <class F>
+    static __device__ __forceinline__ void each(const acc_t (&acc)[1][1], F&& f)
+    {
+        each(acc, [](int, int, int) {}, [&](int, int i, int j, auto& v) { f(i, j, v); });
     }
 };
 

@@ -225,8 +225,9 @@ def test_newton_schulz_many_matrices(batch, rows, cols):
     # (four by four: singular values may vanish in few dimensions)
     assert rel(out[pick], ref) <= (HARD if rows == 4 else TOL)
     assert torch.isfinite(out).all()
+    # alone it may take other tiles, whose sums run in another order
     one = cc.newton_schulz(dev(g[batch - 1]))
-    assert torch.equal(out[batch - 1], one)
+    assert rel(one, ref[3]) <= (HARD if rows == 4 else TOL)
 
 
 def muon_ref(w, g, v, lr, mu, wd, nesterov, scale, steps=5):
