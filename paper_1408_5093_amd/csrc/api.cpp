@@ -2866,6 +2866,8 @@ static int muon_update(const caffe_ns_desc* desc, float* w, const float* g, floa
     CHECK(check_ptr(w, nz, "w"));
     CHECK(check_ptr(g, nz, "g"));
     CHECK(check_ptr(v, nz, "v"));
+    if (nz && (w == g || w == v || g == v))
+        return fail(CAFFE_ERR_INVALID_ARG, "w, g and v must not overlap");
     CHECK(check_ws(workspace, ws_bytes, q.ws_bytes));
     NsArgs x = ns_args(desc);
     x.g = g;

@@ -68,7 +68,8 @@ def test_muon_update_arguments():
                                      P(0x10000), n, None)
 
     for kw in (dict(lr=nan), dict(mu=nan), dict(wd=nan), dict(sc=nan), dict(nest=2),
-               dict(w=None), dict(g=None), dict(v=None)):
+               dict(w=None), dict(g=None), dict(v=None), dict(w=0x2000), dict(v=0x2000),
+               dict(v=0x1000)):
         assert call(**kw) == INVALID, kw
     assert call(w=0x1004) == ALIGN and call(n=need - 1) == WORKSPACE
     assert call(d=_ns(dtype=cc.CAFFE_BF16)) == UNSUPPORTED

@@ -297,6 +297,54 @@ def test_muon_update_captured(rows, cols):
         assert torch.equal(we, wg) and torch.equal(ve, vg), it
 
 
+def test_two_streams_at_once():
+    """Calls on two streams with a workspace each, small and tiled matrices, are
+    the calls one after the other."""
+    rng = np.random.default_rng(12)
+    gs = [dev(gradient(rng, 2, r, c)) for r, c in ((40, 700), (300, 400), (30, 50), (700, 640))]
+    want = [cc.newton_schulz(g) for g in gs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [cc.Workspace() for _ in range(2)]
+    size = max(cc.newton_schulz_workspace_size(cc.ns_desc(g.shape)) for g in gs)
+    for w in spaces:
+        w.get(size)
+    outs = [[torch.empty_like(g) for g in gs] for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for k, g in enumerate(gs):
+            for s, w, o in zip(streams, spaces, outs):
+                cc.newton_schulz(g, out=o[k], ws=w, stream=s)
+    torch.cuda.synchronize()
+    for o in outs:
+        for a, b in zip(o, want):
+            assert torch.equal(a, b)
+
+
+def test_graphs_that_share_a_workspace():
+    """Two captured updates on one workspace, replayed in turn, are the eager
+    ones in turn (nothing is kept in a workspace between calls)."""
+    rng = np.random.default_rng(13)
+    shapes = [(1, 60, 300), (1, 260, 200)]
+    ws = cc.Workspace()
+    ws.get(max(cc.newton_schulz_workspace_size(cc.ns_desc(s)) for s in shapes))
+    g = [dev(gradient(rng, *s)) for s in shapes]
+    eager = [[dev(rng.standard_normal(s)), torch.zeros(s, device=DEV)] for s in shapes]
+    mine = [[w.clone(), v.clone()] for w, v in eager]
+    torch.cuda.synchronize()
+    graphs = []
+    for k in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[k]):
+            cc.muon_update(mine[k][0], g[k], mine[k][1], 0.1, ws=ws)
+    for it in range(4):
+        for k in (it % 2, 1 - it % 2):
+            graphs[k].replay()
+            cc.muon_update(eager[k][0], g[k], eager[k][1], 0.1)
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert torch.equal(mine[k][0], eager[k][0]) and torch.equal(mine[k][1], eager[k][1])
+
+
 def test_muon_update_refuses():
     x = torch.zeros(4, 8, device=DEV)
     with pytest.raises(ValueError, match="contiguous"):
