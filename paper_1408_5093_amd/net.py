@@ -230,6 +230,7 @@ class ConvStack:
                                            r["k"])
         # (q, scale) of the layers held in 8 bits (quantize_inner_products)
         self.int8 = [None] * n
+        self.ws_int8 = Workspace(dev)
         # when a list, (tag, event) pairs are recorded around every conv call:
         # tag = (kind, layer, "begin" | "end") with kind "fwd" (forward),
         # "bwd" (data gradient), "wgt" (weight and bias gradients) or "both"
@@ -256,7 +257,7 @@ class ConvStack:
                 self.lrn_stage_only[l - 1] = False
             need = max(need, self.N * (self.int8[l][0].shape[1] + 4))
             done.append(l)
-        self.ws_int8 = Workspace(self.W[0].device)
+        # (the same memory at every call: a captured forward pass holds it)
         self.ws_int8.get(need)
         return done
 

@@ -147,3 +147,28 @@ def test_bf16_network_scores_in_8_bits():
         q, s = rows_ref(_np(net.bottom[l]).reshape(8, L.C).astype(np.float32))
         p, t = rows_ref(_np(net.W[l].float()).reshape(L.K, L.C).astype(np.float32))
         check_top(net.top[l].view(8, L.K), *ip_ref(q, s, p, t, _np(net.b[l]), L.relu))
+
+
+def test_rows_made_again_under_a_captured_forward():
+    """The rows made again after a forward pass was captured: replays use the new
+    ones, in the memory that the capture saw."""
+    xs, _, net = NETS["lenet"](16)
+    x = torch.from_numpy(xs[0]).to(DEV)
+    ips = net.quantize_inner_products()
+    net.forward(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        top = net.forward(x)
+    held = [net.ws_int8.buf.data_ptr()] + [t.data_ptr() for l in ips for t in net.int8[l]]
+    for it in range(3):
+        for l in ips:
+            net.W[l].mul_(-0.5)
+        net.quantize_inner_products()
+        assert held == [net.ws_int8.buf.data_ptr()] + [t.data_ptr() for l in ips
+                                                       for t in net.int8[l]]
+        want = net.forward(x).clone()
+        top.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(top, want), it
