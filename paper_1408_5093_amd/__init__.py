@@ -549,13 +549,23 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-def _call(index, fn, *args, stream=None):
-    """fn(*args, stream) with device `index` current, on `stream` or its current one."""
+def _elsewhere(stream, t):
+    """Whether `stream` is another than the current one of t's device.  A call on
+    such a stream makes it current first, so that the memory it allocates (a
+    workspace that it drops again, outputs) belongs to that stream."""
+    if stream is None:
+        return False
+    if stream.device_index != t.get_device():
+        raise ValueError(f"the stream is on device {stream.device_index}, the tensors on {t.device}")
+    return stream.cuda_stream != torch._C._cuda_getCurrentRawStream(stream.device_index)
+
+
+def _call(index, fn, *args):
+    """fn(*args, stream) with device `index` current, on its current stream."""
     if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
-            return _call(index, fn, *args, stream=stream)
-    status = fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None
-                else stream.cuda_stream)
+            return _call(index, fn, *args)
+    status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
     if status:
         check(status)
 
@@ -563,6 +573,9 @@ def _call(index, fn, *args, stream=None):
 def newton_schulz(g, steps=5, coef=NS_COEF, eps=1e-7, group=1, out=None, ws=None, stream=None):
     """Each matrix of g (see ns_desc; float32 or bfloat16) brought near its
     nearest semi-orthogonal matrix by `steps` Newton-Schulz products."""
+    if _elsewhere(stream, g):
+        with torch.cuda.stream(stream):
+            return newton_schulz(g, steps, coef, eps, group, out, ws)
     if g.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError(f"in must be float32 or bfloat16, got {g.dtype}")
     _dev(g, "in", g.dtype)
@@ -577,7 +590,7 @@ def newton_schulz(g, steps=5, coef=NS_COEF, eps=1e-7, group=1, out=None, ws=None
     buf = (ws or Workspace(g.device)).get(newton_schulz_workspace_size(d))
     _checked(dev, buf, "workspace", torch.uint8)
     _call(dev, load().caffe_newton_schulz, ctypes.byref(d), g.data_ptr(), out.data_ptr(),
-          _addr(buf), 0 if buf is None else buf.numel(), stream=stream)
+          _addr(buf), 0 if buf is None else buf.numel())
     return out
 
 
@@ -587,6 +600,10 @@ def muon_update(w, g, v, lr, momentum=0.95, weight_decay=0.0, nesterov=True, sca
     w <- w - lr (scale newton_schulz(u) + weight_decay w).  `scale` defaults to
     sqrt(max(1, rows / cols)).  `lr` is a number, or a one-element float32
     device tensor read when the kernel runs (for graph capture)."""
+    if _elsewhere(stream, w):
+        with torch.cuda.stream(stream):
+            return muon_update(w, g, v, lr, momentum, weight_decay, nesterov, scale, steps, coef, eps,
+                               group, ws)
     _dev(w, "w", torch.float32)
     dev = w.get_device()
     _checked(dev, g, "g", torch.float32), _checked(dev, v, "v", torch.float32)
@@ -605,8 +622,7 @@ def muon_update(w, g, v, lr, momentum=0.95, weight_decay=0.0, nesterov=True, sca
     _call(dev, load().caffe_muon_update_device_lr if on_device else load().caffe_muon_update,
           ctypes.byref(d), w.data_ptr(), g.data_ptr(), v.data_ptr(),
           lr.data_ptr() if on_device else float(lr), float(momentum), float(weight_decay),
-          float(scale), int(bool(nesterov)), _addr(buf), 0 if buf is None else buf.numel(),
-          stream=stream)
+          float(scale), int(bool(nesterov)), _addr(buf), 0 if buf is None else buf.numel())
 
 
 # ------------------------------------------------------------- 8-bit rows
@@ -631,6 +647,9 @@ def quantize_rows(x, q=None, scale=None, stream=None):
     """x (rows, ...) float32 or bfloat16, e.g. an inner product's weight or its
     bottom -> (q, scale): int8 rows padded with zeros to int8_pitch(cols)
     bytes, and float32 scales, with x[r] near q[r, :cols] * scale[r]."""
+    if _elsewhere(stream, x):
+        with torch.cuda.stream(stream):
+            return quantize_rows(x, q, scale)
     kind = _ROW_TYPES.get(x.dtype)
     if kind is None:
         raise ValueError(f"x must be float32 or bfloat16, got {x.dtype}")
@@ -647,7 +666,7 @@ def quantize_rows(x, q=None, scale=None, stream=None):
     if q.shape != (rows, pitch) or scale.numel() != rows:
         raise ValueError(f"q must be {(rows, pitch)} and scale {(rows,)}")
     _call(dev, load().caffe_quantize_rows, x.data_ptr(), kind, rows, cols, q.data_ptr(),
-          scale.data_ptr(), stream=stream)
+          scale.data_ptr())
     return q, scale
 
 
@@ -657,6 +676,10 @@ def inner_product_int8(x, weight, weight_scale, bias=None, C=None, x_scale=None,
     quantize_rows makes them; x (N, ...) of C values a sample in float32 or
     bfloat16 (brought to 8-bit rows in the call), or int8 rows with x_scale.
     C (the values of a row) may be left out for a float x."""
+    if _elsewhere(stream, x):
+        with torch.cuda.stream(stream):
+            return inner_product_int8(x, weight, weight_scale, bias, C, x_scale, relu, top_dtype,
+                                      out, ws)
     kind = CAFFE_INT8_ROWS if x.dtype is torch.int8 else _ROW_TYPES.get(x.dtype)
     if kind is None:
         raise ValueError(f"bottom must be float32, bfloat16 or int8, got {x.dtype}")
@@ -701,6 +724,5 @@ def inner_product_int8(x, weight, weight_scale, bias=None, C=None, x_scale=None,
             _checked(dev, buf, "workspace", torch.uint8)
             buf, buf_bytes = buf.data_ptr(), buf.numel()
     _call(dev, lib.caffe_inner_product_int8, desc, x.data_ptr(), _addr(x_scale),
-          weight.data_ptr(), weight_scale.data_ptr(), _addr(bias), out.data_ptr(), buf, buf_bytes,
-          stream=stream)
+          weight.data_ptr(), weight_scale.data_ptr(), _addr(bias), out.data_ptr(), buf, buf_bytes)
     return out

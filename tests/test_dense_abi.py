@@ -187,3 +187,16 @@ def test_host_tensors_and_shapes_are_refused():
                                             torch.zeros(3))):
         with pytest.raises(ValueError):
             f()
+
+
+def test_streams_of_another_device_are_refused():
+    class Other:
+        device_index, cuda_stream = 1, 0x1000
+
+    x = torch.zeros(4, 8)
+    q, t = torch.zeros(3, 128, dtype=torch.int8), torch.zeros(3)
+    for f in (lambda s: cc.newton_schulz(x, stream=s), lambda s: cc.quantize_rows(x, stream=s),
+              lambda s: cc.muon_update(x, x.clone(), x.clone(), 0.1, stream=s),
+              lambda s: cc.inner_product_int8(x, q, t, stream=s)):
+        with pytest.raises(ValueError, match="stream"):
+            f(Other())

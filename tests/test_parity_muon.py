@@ -357,3 +357,39 @@ def test_muon_update_refuses():
         cc.muon_update(x, x.bfloat16(), x.clone(), 0.1)
     with pytest.raises(cc.CaffeError, match="ALIGN"):
         cc.newton_schulz(torch.zeros(33, device=DEV)[1:].view(4, 8))
+
+
+def test_memory_of_a_call_belongs_to_its_stream(monkeypatch):
+    """With stream=, the workspace that a call drops again and its outputs are
+    that stream's memory: the current stream is not given them while the call
+    may still run."""
+    taken = []
+    get = cc.Workspace.get
+
+    def noted(self, nbytes):
+        buf = get(self, nbytes)
+        taken.append((buf.data_ptr(), buf.numel()))
+        return buf
+
+    monkeypatch.setattr(cc.Workspace, "get", noted)
+    rng = np.random.default_rng(14)
+    g = dev(gradient(rng, 2, 300, 400))
+    x = dev(rng.standard_normal((40, 900)))
+    w, v = g.clone(), torch.zeros_like(g)
+    q, t = cc.quantize_rows(x)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    outs = [cc.newton_schulz(g, stream=s), cc.inner_product_int8(x, q, t, stream=s),
+            *cc.quantize_rows(x, stream=s)]
+    cc.muon_update(w, g, v, 0.1, stream=s)
+    assert len(taken) == 3
+    mine = [torch.empty(n, dtype=torch.uint8, device=DEV) for _ in range(2) for _, n in taken]
+    for a, n in taken:
+        for b in mine:
+            assert b.data_ptr() + b.numel() <= a or a + n <= b.data_ptr()
+    torch.cuda.synchronize()
+    w2, v2 = g.clone(), torch.zeros_like(g)
+    cc.muon_update(w2, g, v2, 0.1)
+    for a, b in zip(outs + [w, v], [cc.newton_schulz(g), cc.inner_product_int8(x, q, t), q, t,
+                                    w2, v2]):
+        assert torch.equal(a, b)
