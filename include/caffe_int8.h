@@ -22,8 +22,8 @@
  * Conventions (memory, streams, errors, status codes) are those of
  * caffe_conv.h: caller-owned 16-byte-aligned device pointers, a 256-byte
  * aligned workspace, asynchronous execution on `stream`, negative
- * caffe_status on failure with nothing enqueued, no atomics.  Tensors may
- * exceed 2^31 bytes.
+ * caffe_status on failure with nothing enqueued, no atomics.  What a call
+ * writes overlaps none of its other buffers.  Tensors may exceed 2^31 bytes.
  */
 #ifndef CAFFE_INT8_H
 #define CAFFE_INT8_H
@@ -64,9 +64,9 @@ int caffe_quantize_rows(const void* x, int32_t dtype, int64_t rows, int32_t cols
 int caffe_inner_product_int8_workspace_size(const caffe_ip8_desc* desc, size_t* bytes);
 
 /* N and K are at most 2^26, N x K at most 2^23 tiles of 64 x 64 (else
- * CAFFE_ERR_UNSUPPORTED).  bottom: N x C values, or with CAFFE_INT8_ROWS N 8-bit rows and bottom_scale
- * (N floats; NULL otherwise).  weight: K 8-bit rows with weight_scale (K
- * floats).  bias: K floats or NULL. */
+ * CAFFE_ERR_UNSUPPORTED).  bottom: N x C values, or with CAFFE_INT8_ROWS N
+ * 8-bit rows and bottom_scale (N floats; NULL otherwise).  weight: K 8-bit
+ * rows with weight_scale (K floats).  bias: K floats or NULL. */
 int caffe_inner_product_int8(const caffe_ip8_desc* desc, const void* bottom,
                              const float* bottom_scale, const int8_t* weight,
                              const float* weight_scale, const float* bias, void* top,

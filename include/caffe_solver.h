@@ -129,7 +129,7 @@ typedef struct caffe_ns_desc {
  * (a diverging iteration). */
 int caffe_newton_schulz_workspace_size(const caffe_ns_desc* desc, size_t* bytes);
 
-/* out = NS(in) for each matrix.  out may be in. */
+/* out = NS(in) for each matrix.  out may be in, else they must not overlap. */
 int caffe_newton_schulz(const caffe_ns_desc* desc, const void* in, void* out, void* workspace,
                         size_t ws_bytes, void* stream);
 

@@ -2812,6 +2812,14 @@ static int plan_ns(const caffe_ns_desc* d, NsPlan* q)
     return CAFFE_OK;
 }
 
+// whether two blobs of the batch share memory
+static bool ns_overlap(const caffe_ns_desc* d, const void* x, const void* y)
+{
+    const uint64_t size = (uint64_t)d->batch * d->rows * d->cols * (d->dtype == CAFFE_BF16 ? 2 : 4);
+    const uint64_t a = (uint64_t)x, b = (uint64_t)y;
+    return (a < b ? b - a : a - b) < size;
+}
+
 static NsArgs ns_args(const caffe_ns_desc* d)
 {
     NsArgs x{};
@@ -2841,6 +2849,8 @@ int caffe_newton_schulz(const caffe_ns_desc* desc, const void* in, void* out, vo
     CHECK(check_ptr(in, q.batch > 0, "in"));
     CHECK(check_ptr(out, q.batch > 0, "out"));
     CHECK(check_ws(workspace, ws_bytes, q.ws_bytes));
+    if (in != out && ns_overlap(desc, in, out))
+        return fail(CAFFE_ERR_INVALID_ARG, "out must be in or not overlap it");
     NsArgs x = ns_args(desc);
     x.g = in;
     x.out = out;
@@ -2866,9 +2876,9 @@ static int muon_update(const caffe_ns_desc* desc, float* w, const float* g, floa
     CHECK(check_ptr(w, nz, "w"));
     CHECK(check_ptr(g, nz, "g"));
     CHECK(check_ptr(v, nz, "v"));
-    if (nz && (w == g || w == v || g == v))
-        return fail(CAFFE_ERR_INVALID_ARG, "w, g and v must not overlap");
     CHECK(check_ws(workspace, ws_bytes, q.ws_bytes));
+    if (ns_overlap(desc, w, g) || ns_overlap(desc, w, v) || ns_overlap(desc, g, v))
+        return fail(CAFFE_ERR_INVALID_ARG, "w, g and v must not overlap");
     NsArgs x = ns_args(desc);
     x.g = g;
     x.v = v;

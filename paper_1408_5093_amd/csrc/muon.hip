@@ -206,8 +206,8 @@ __device__ __forceinline__ void tile_at(int t, int mt, int nt, int& I, int& J)
 }
 
 // 32 x 32 by four waves that share the reduction, 64 x 64 and 128 x 128 by 2 x 2
-// waves, all with accumulators for the low terms; 192 x 192 by four waves and 256 x 192 by eight, whose accumulators fill the
-// registers.
+// waves, all with accumulators for the low terms; 192 x 192 by four waves and
+// 256 x 192 by eight, whose accumulators fill the registers.
 typedef TileNT<OpPairLine, 2, 2, 1, 1, 5, true> Tile64;
 typedef TileShared<OpPairLine, 4, true> Tile32;
 typedef TileNT<OpPair, 2, 2, 2, 2, 2, true> Tile128;

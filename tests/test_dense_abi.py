@@ -200,3 +200,17 @@ def test_streams_of_another_device_are_refused():
               lambda s: cc.inner_product_int8(x, q, t, stream=s)):
         with pytest.raises(ValueError, match="stream"):
             f(Other())
+
+
+def test_blobs_that_overlap_in_part():
+    """2 x 20 x 30 floats are 4800 bytes (0x12C0)."""
+    lib = cc.load()
+    d = _ns()
+    need = cc.newton_schulz_workspace_size(d)
+    for i, o in ((0x8000, 0x8010), (0x8010, 0x8000), (0x8000, 0x92B0), (0x92B0, 0x8000)):
+        assert lib.caffe_newton_schulz(ctypes.byref(d), P(i), P(o), P(0x10000), need,
+                                       None) == INVALID, (i, o)
+    far = 0x80000
+    for w, g, v in ((0x8000, 0x92B0, far), (0x8000, far, 0x8010), (far, 0x92B0, 0x8000)):
+        assert lib.caffe_muon_update(ctypes.byref(d), P(w), P(g), P(v), 0.1, 0.9, 0.0, 1.0, 1,
+                                     P(0x10000), need, None) == INVALID, (w, g, v)

@@ -393,3 +393,18 @@ def test_memory_of_a_call_belongs_to_its_stream(monkeypatch):
     for a, b in zip(outs + [w, v], [cc.newton_schulz(g), cc.inner_product_int8(x, q, t), q, t,
                                     w2, v2]):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("shape", [(2, 20, 30), (1, 132, 200)])
+def test_blobs_next_to_each_other(shape):
+    """Blobs without a gap between them do not overlap."""
+    rng = np.random.default_rng(15)
+    g = gradient(rng, *shape)
+    near = torch.zeros(4, *shape, device=DEV)
+    near[0], near[2] = 1.0, dev(g)
+    w, v = torch.ones(shape, device=DEV), torch.zeros(shape, device=DEV)
+    cc.muon_update(w, dev(g), v, 0.1)
+    cc.muon_update(near[0], near[2], near[1], 0.1)
+    cc.newton_schulz(near[2], out=near[3])
+    assert torch.equal(near[0], w) and torch.equal(near[1], v)
+    assert torch.equal(near[2], dev(g)) and torch.equal(near[3], cc.newton_schulz(dev(g)))
