@@ -39,7 +39,10 @@
  *   X <- a X + (b A + c A A) X,  A = X X^T,  `steps` times
  * NS of a zero matrix is zero; a NaN or an infinity in U makes the whole
  * NS(U) NaN.  Its arithmetic is that of float operands: half-precision pairs
- * of 22 bits, float sums (errors of the float output near 1e-6 of its norm).
+ * of 22 bits, float sums.  With the usual coefficients and 3 to 6 steps the
+ * float output was within 6e-6 of its norm over 700 shapes.  With a side of at
+ * most 128 that can be several times the error of steps one by one in float
+ * (10 x 16: 5.1e-6, they 0.8e-6); beyond it is like theirs.
  * The pairs hold a fixed range: an element of X_0 has an absolute error of
  * 2^-39, so parts of U more than 2^20 below ||U||_F + eps lose relative
  * accuracy.
