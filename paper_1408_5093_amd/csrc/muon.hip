@@ -559,9 +559,10 @@ bool ns_plan(int batch, int rows, int cols, int steps, float a, float b, float c
     // the longest first segment, and the longest later one
     int first = steps, later = steps;
     if (qall > 1.0) {
+        // (as doubles: for qall next to 1 the quotients pass every int)
         const double per = 2.0 * log(qall);
-        first = std::min(steps, 1 + (int)floor(log(256.0) / per + 1e-9));
-        later = std::min(steps, 1 + (int)floor(log(16.0) / per + 1e-9));
+        first = (int)std::min((double)steps, 1 + floor(log(256.0) / per + 1e-9));
+        later = (int)std::min((double)steps, 1 + floor(log(16.0) / per + 1e-9));
     }
     q->segments = 1 + (steps - first + later - 1) / later;
     int left = steps;

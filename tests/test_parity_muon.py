@@ -408,3 +408,21 @@ def test_blobs_next_to_each_other(shape):
     cc.newton_schulz(near[2], out=near[3])
     assert torch.equal(near[0], w) and torch.equal(near[1], v)
     assert torch.equal(near[2], dev(g)) and torch.equal(near[3], cc.newton_schulz(dev(g)))
+
+
+SMALL_SEGMENTS_TILES = [(1, 20, 30), (2, 50, 500), (1, 192, 300)]  # one launch, slabs, tiles
+
+
+@pytest.mark.parametrize("shape", SMALL_SEGMENTS_TILES)
+@pytest.mark.parametrize("coef,steps", [((1.0, 1e-9, 0.0), 5), ((1.0, 1e-9, 0.0), 64),
+                                        ((1.0, 1e-30, 1e-30), 7), ((1.0, 2e-9, 0.0), 5)])
+def test_coefficients_next_to_the_identity(shape, coef, steps):
+    """|q| just above 1, where steps of any number make one segment."""
+    print(f"next to the identity {shape} {coef} x {steps}", flush=True)
+    g = gradient(np.random.default_rng([16, steps]), *shape)
+    x = dev(g)
+    out = cc.newton_schulz(x, steps, coef, out=torch.full_like(x, float("nan")))
+    assert rel(out, ns_ref(g, steps, coef)) <= TOL
+    w, v = torch.zeros_like(x), torch.zeros_like(x)
+    cc.muon_update(w, x, v, 1.0, 0.0, nesterov=False, scale=1.0, steps=steps, coef=coef)
+    assert rel(-w, ns_ref(g, steps, coef)) <= TOL and torch.equal(v, x)
