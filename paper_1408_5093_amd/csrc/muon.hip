@@ -516,14 +516,15 @@ static void ns_ranges(double a, double b, double c, double top, double* qmax, do
     if (c != 0.0)
         at[n++] = -b / (2 * c);
     // d/dt t q^2 = q (q + 2 t q'):  a + 3 b t + 5 c t^2 = 0 (q = 0 gives the minimum)
-    if (c != 0.0) {
-        const double d = 9 * b * b - 20 * a * c;
-        if (d >= 0) {
-            at[n++] = (-3 * b + sqrt(d)) / (10 * c);
-            at[n++] = (-3 * b - sqrt(d)) / (10 * c);
-        }
-    } else if (b != 0.0) {
-        at[n++] = -a / (3 * b);
+    // with the root that does not cancel formed by the quadratic formula and the
+    // other from the product of both, a / (5 c): right for c of any size, also 0
+    const double d = 9 * b * b - 20 * a * c;
+    if (d >= 0) {
+        const double w = -0.5 * (3 * b + copysign(sqrt(d), b));
+        if (c != 0.0)
+            at[n++] = w / (5 * c);
+        if (w != 0.0)
+            at[n++] = a / w;
     }
     *qmax = *tmax = 0.0;
     for (int i = 0; i < n; ++i)

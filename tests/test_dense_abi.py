@@ -214,3 +214,14 @@ def test_blobs_that_overlap_in_part():
     for w, g, v in ((0x8000, 0x92B0, far), (0x8000, far, 0x8010), (far, 0x92B0, 0x8000)):
         assert lib.caffe_muon_update(ctypes.byref(d), P(w), P(g), P(v), 0.1, 0.9, 0.0, 1.0, 1,
                                      P(0x10000), need, None) == INVALID, (w, g, v)
+
+
+def test_range_of_coefficients_with_a_vanishing_third():
+    """t (90 - 90 t)^2 has its largest value, 1200, inside [0, 1]: refused however
+    small the coefficient of t^2 is."""
+    for c in (0.0, 1e-17, -1e-17, 1e-30, 1e-9):
+        with pytest.raises(cc.CaffeError, match="range"):
+            cc.newton_schulz_workspace_size(cc.ns_desc((64, 64), 1, (90.0, -90.0, c)))
+    # 5 c t^2 + 3 b t + a with b = 0: its root is a range's end or outside
+    for coef in ((1.0, 0.0, -1.0), (0.5, 0.0, 0.25), (0.0, 1.0, 0.0), (0.0, 0.0, 1.0)):
+        assert cc.newton_schulz_workspace_size(cc.ns_desc((64, 64), 3, coef)) > 0

@@ -426,3 +426,13 @@ def test_coefficients_next_to_the_identity(shape, coef, steps):
     w, v = torch.zeros_like(x), torch.zeros_like(x)
     cc.muon_update(w, x, v, 1.0, 0.0, nesterov=False, scale=1.0, steps=steps, coef=coef)
     assert rel(-w, ns_ref(g, steps, coef)) <= TOL and torch.equal(v, x)
+
+
+@pytest.mark.parametrize("shape", SMALL_SEGMENTS_TILES)
+@pytest.mark.parametrize("c", [1e-17, -1e-25])
+def test_range_of_coefficients_with_a_vanishing_third(shape, c):
+    """t (2.9 - 2.9 t)^2 is largest inside [0, 1] (1.25) and vanishes at both ends."""
+    print(f"vanishing third {shape} {c}", flush=True)
+    g = gradient(np.random.default_rng(17), *shape, rank=1, noise=0.5)
+    coef = (2.9, -2.9, c)
+    assert rel(cc.newton_schulz(dev(g), 2, coef), ns_ref(g, 2, coef)) <= TOL
