@@ -45,7 +45,8 @@
  * (10 x 16: 5.1e-6, they 0.8e-6); beyond it is like theirs.
  * The pairs hold a fixed range: an element of X_0 has an absolute error of
  * 2^-39, so parts of U more than 2^20 below ||U||_F + eps lose relative
- * accuracy.
+ * accuracy; so does the result of coefficients whose steps shrink it below
+ * 2^-96.
  *
  * Learning-rate schedules at iteration t >= 0 (0 for the first update),
  * evaluated on the host in double precision:

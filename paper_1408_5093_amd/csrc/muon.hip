@@ -575,7 +575,8 @@ bool ns_plan(int batch, int rows, int cols, int steps, float a, float b, float c
     for (int i = 0, k = 0; i < q->segments; ++i) {
         double pb = 1.0;
         for (int l = 0; l < q->length[i]; ++l, ++k)
-            q->pmax[k] = pb = std::max(pb * q->qmax[k], 1e-9);
+            // (the scale 2^-e of a product, e <= 109, and of X in it are floats)
+            q->pmax[k] = pb = std::max(pb * q->qmax[k], 0x1p-96);
     }
     const size_t align = 255;
     const size_t mp = (size_t)((q->m + 31) / 32) * 128, np = (size_t)((q->n + 31) / 32) * 128;

@@ -436,3 +436,13 @@ def test_range_of_coefficients_with_a_vanishing_third(shape, c):
     g = gradient(np.random.default_rng(17), *shape, rank=1, noise=0.5)
     coef = (2.9, -2.9, c)
     assert rel(cc.newton_schulz(dev(g), 2, coef), ns_ref(g, 2, coef)) <= TOL
+
+
+@pytest.mark.parametrize("shape", SMALL_SEGMENTS_TILES)
+@pytest.mark.parametrize("coef,steps", [((0.1, 0.02, 0.0), 20), ((0.25, 0.0, 0.0), 40),
+                                        ((0.01, 0.0, 0.0), 12)])
+def test_coefficients_that_shrink(shape, coef, steps):
+    """Products of q down to 2^-96 keep the operands' bits."""
+    print(f"shrinking {shape} {coef} x {steps}", flush=True)
+    g = gradient(np.random.default_rng([18, steps]), *shape)
+    assert rel(cc.newton_schulz(dev(g), steps, coef), ns_ref(g, steps, coef)) <= TOL
