@@ -18,18 +18,21 @@ typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 // inv = fl(1 / s), is within 127 * 2^-23 < 2^-16 of the quotient, so its
 // rounding is the quotient's unless it lies within 2^-15 of a half.  There the
 // rounded quotient t = fl(x / s) decides: it is on the same side of the half as
-// x / s, or on the half itself, and then the remainder x - t s (exact in one
-// fma) says on which side the quotient was.
+// x / s, or on the half itself, and then the remainder x - t s says on which
+// side the quotient was.  The remainder is a multiple of half a unit of s and
+// less than 2^8 of them, exact in one fma where that half is a float: x and s
+// below 2^-100 are taken 2^64 times.
 __device__ __forceinline__ int round_quotient(float x, float s, float inv)
 {
     const float near = x * inv;
     float r = rintf(near);
     if (!(fabsf(fabsf(near - r) - 0.5f) > 0x1p-15f)) {  // (also where inv overflows)
-        const float t = x / s;
+        const float up = s < 0x1p-100f ? 0x1p64f : 1.f;  // exact: |x| < 2^7 s
+        const float xs = x * up, ss = s * up, t = xs / ss;
         r = rintf(t);
         const float d = t - r;  // exact
         if (fabsf(d) == 0.5f) {
-            const float rem = fmaf(-t, s, x);
+            const float rem = fmaf(-t, ss, xs);
             // toward the side of the quotient (s > 0); the even one at rem = 0
             if (rem > 0.f && d > 0.f)
                 r += 1.f;

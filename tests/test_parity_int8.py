@@ -270,3 +270,36 @@ def test_refusals():
         cc.quantize_rows(x[0])
     with pytest.raises(ValueError):
         cc.quantize_rows(x, q=q[:, :100])
+
+
+def test_quantize_rows_at_halves_of_subnormal_scales():
+    """Scales S 2^-149: the floats next to a half of one on both sides, where the
+    quotient may be off the half by less than a float's remainder can tell."""
+    rng = np.random.default_rng(28)
+    unit = 2.0 ** -149
+    for S in [1, 2, 3, 255, 131073, 951315, (1 << 23) - 1, (1 << 23) + 1, (1 << 24) - 1,
+              *(int(v) for v in np.exp(rng.uniform(np.log(1 << 16), np.log(1 << 26), 300)))]:
+        top = np.float32(127.0 * S * unit)
+        s = int(float(np.float32(float(top) / 127)) / unit)
+        k = 2 * rng.integers(0, 127, 60) + 1
+        near = np.concatenate([(k * s + e) // 2 for e in (-3, -1, 0, 1, 3)]).astype(np.float64)
+        x = np.concatenate([[top], near * unit, -near * unit]).astype(np.float32)[None]
+        x = np.clip(x, -top, top)
+        check_rows(*cc.quantize_rows(dev(x)), x)
+    # the same in bfloat16
+    top = np.float32(2.0 ** -124 * 1.921875)
+    x = np.float32([[top, top / 2, -top / 2, top / 4, top * 0.75]])
+    xb = dev(x, torch.bfloat16)
+    check_rows(*cc.quantize_rows(xb), xb.float().cpu().numpy())
+
+
+def test_products_of_rows_with_subnormal_scales():
+    """One sample (rounded in the product's own launch) is the row that
+    quantize_rows makes."""
+    top = float.fromhex("0x1.fc00fep-126")
+    x = np.float32([[top, float.fromhex("0x1.020082p-126"), 0.0, -top]])
+    q, s = rows_ref(x)
+    assert q[0, 1] == 65
+    w, t = cc.quantize_rows(dev(np.eye(4, dtype=np.float32) * 127))
+    y = cc.inner_product_int8(dev(x), w, t)
+    assert np.array_equal(y.cpu().numpy(), (q.astype(np.float32) * 127) * s[0])
