@@ -99,18 +99,37 @@ def _dev(t, name, dtype=None):
 
 
 class Workspace:
-    """A growable device byte buffer for the library's scratch space."""
+    """A growable device byte buffer for the library's scratch space.
+
+    A buffer that is too small is dropped for a larger one.  Its memory then
+    waits for every stream that a call took it on (the current stream at
+    get()); one that was taken under capture is kept, since the graph's replays
+    go on writing it.  A Workspace has to live as long as such graphs."""
 
     def __init__(self, device=None):
         self.device = device
         self.buf = None
+        self._streams = ()  # raw handles of the streams that the buffer is known to
+        self._captured = False
+        self._kept = []
 
     def get(self, nbytes):
         if nbytes == 0:
             return None
-        if self.buf is None or self.buf.numel() < nbytes:
-            self.buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device or "cuda")
-        return self.buf
+        buf = self.buf
+        if buf is None or buf.numel() < nbytes:
+            if self._captured:
+                self._kept.append(buf)
+            buf = self.buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device or "cuda")
+            self._streams = (torch._C._cuda_getCurrentRawStream(buf.get_device()),)
+            self._captured = False
+        raw = torch._C._cuda_getCurrentRawStream(buf.get_device())
+        if raw not in self._streams:
+            buf.record_stream(torch.cuda.current_stream(buf.get_device()))
+            self._streams += (raw,)
+        if not self._captured:
+            self._captured = torch.cuda.is_current_stream_capturing()
+        return buf
 
 
 def _op_dtype(desc):

@@ -2,6 +2,8 @@
 invalid argument becomes its status code before any GPU work, and the
 workspace queries answer without a GPU."""
 import ctypes
+import gc
+import weakref
 
 import pytest
 import torch
@@ -225,3 +227,68 @@ def test_range_of_coefficients_with_a_vanishing_third():
     # 5 c t^2 + 3 b t + a with b = 0: its root is a range's end or outside
     for coef in ((1.0, 0.0, -1.0), (0.5, 0.0, 0.25), (0.0, 1.0, 0.0), (0.0, 0.0, 1.0)):
         assert cc.newton_schulz_workspace_size(cc.ns_desc((64, 64), 3, coef)) > 0
+
+
+class _Buffer:
+    """A device buffer that notes the streams it is recorded on."""
+
+    def __init__(self, n):
+        self.n, self.streams = n, []
+
+    def numel(self):
+        return self.n
+
+    def get_device(self):
+        return 0
+
+    def record_stream(self, s):
+        self.streams.append(s)
+
+
+@pytest.fixture
+def fake_device(monkeypatch):
+    """(state, buffers): state holds the current raw stream and whether it captures."""
+    state, made = dict(raw=1, capturing=False), []
+
+    def empty(n, **kw):
+        made.append(_Buffer(n))
+        return made[-1]
+
+    monkeypatch.setattr(torch, "empty", empty)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: state["raw"])
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda i=None: state["raw"])
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: state["capturing"])
+    return state, made
+
+
+def test_workspace_is_recorded_on_the_streams_that_take_it(fake_device):
+    """A buffer that a larger one replaces was recorded on every stream but its own
+    that got it, once each: its memory waits for them."""
+    state, made = fake_device
+    ws = cc.Workspace()
+    for raw, n in ((1, 10), (2, 10), (1, 5), (2, 10), (3, 7), (2, 100), (1, 100), (1, 1000)):
+        state["raw"] = raw
+        assert ws.get(n).numel() >= n
+    assert ws.get(0) is None
+    assert [b.n for b in made] == [10, 100, 1000]
+    assert [b.streams for b in made] == [[2, 3], [1], []]
+
+
+def test_workspace_keeps_what_a_graph_writes(fake_device):
+    """A buffer that a capture took outlives its replacement, others do not."""
+    state, made = fake_device
+    ws = cc.Workspace()
+    ws.get(10)
+    ws.get(20)  # (the 10 bytes are dropped)
+    state["capturing"] = True
+    ws.get(15)
+    state["capturing"] = False
+    ws.get(20), ws.get(30), ws.get(40)
+    state["capturing"] = True
+    ws.get(50)  # made under capture
+    state["capturing"] = False
+    ws.get(60), ws.get(70)
+    refs = [weakref.ref(b) for b in made]
+    made.clear()
+    gc.collect()
+    assert [r().n for r in refs if r() is not None] == [20, 50, 70] and ws.buf.n == 70

@@ -446,3 +446,57 @@ def test_coefficients_that_shrink(shape, coef, steps):
     print(f"shrinking {shape} {coef} x {steps}", flush=True)
     g = gradient(np.random.default_rng([18, steps]), *shape)
     assert rel(cc.newton_schulz(dev(g), steps, coef), ns_ref(g, steps, coef)) <= TOL
+
+
+def test_workspace_grown_on_another_stream():
+    """A kept workspace that a call on another stream replaces by a larger one: the
+    first stream is not given its memory while that stream still works."""
+    rng = np.random.default_rng(19)
+    small, large = dev(gradient(rng, 1, 40, 700)), torch.randn((2048, 2048), device=DEV)
+    want = cc.newton_schulz(small), cc.newton_schulz(large)
+    ws, s = cc.Workspace(), torch.cuda.Stream()
+    cc.newton_schulz(small, ws=ws)
+    torch.cuda.synchronize()
+    at, n = ws.buf.data_ptr(), ws.buf.numel()
+    outs = [torch.empty_like(large) for _ in range(10)]
+    out = torch.empty_like(small)
+    torch.cuda.synchronize()
+    busy = cc.Workspace()
+    for o in outs:
+        cc.newton_schulz(large, out=o, ws=busy, stream=s)
+    cc.newton_schulz(small, out=out, ws=ws, stream=s)
+    cc.newton_schulz(large, out=outs[0], ws=ws, stream=s)  # grows
+    mine = [torch.empty(n, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    still = not s.query()  # (a host held up for tens of ms proves nothing)
+    torch.cuda.synchronize()
+    assert ws.buf.numel() > n
+    for t in mine if still else ():
+        assert t.data_ptr() + n <= at or at + n <= t.data_ptr()
+    assert torch.equal(out, want[0])
+    for o in outs:
+        assert torch.equal(o, want[1])
+
+
+def test_workspace_grown_after_a_capture():
+    """A larger call after a capture on the same workspace: replays write neither
+    what was allocated since nor read it."""
+    rng = np.random.default_rng(20)
+    small, large = dev(gradient(rng, 1, 40, 700)), dev(gradient(rng, 1, 700, 900))
+    x, out, ws = small.clone(), torch.empty_like(small), cc.Workspace()
+    cc.newton_schulz(x, out=out, ws=ws)
+    torch.cuda.synchronize()
+    n = ws.buf.numel()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cc.newton_schulz(x, out=out, ws=ws)
+    cc.newton_schulz(large, ws=ws)
+    assert ws.buf.numel() > n
+    mine = [torch.full((n,), 255, dtype=torch.uint8, device=DEV) for _ in range(8)]
+    for it in range(3):
+        x.copy_(small * (it + 1))
+        out.zero_()
+        graph.replay()
+        eager = cc.newton_schulz(x)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager), it
+        assert all(int((t != 255).sum()) == 0 for t in mine), it
