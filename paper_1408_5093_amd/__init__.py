@@ -689,6 +689,12 @@ def quantize_rows(x, q=None, scale=None, stream=None):
     return q, scale
 
 
+def inner_product_int8_workspace_size(desc):
+    n = ctypes.c_size_t()
+    check(load().caffe_inner_product_int8_workspace_size(ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
 def inner_product_int8(x, weight, weight_scale, bias=None, C=None, x_scale=None, relu=False,
                        top_dtype=torch.float32, out=None, ws=None, stream=None):
     """top (N, K) = x weight^T + bias, in 8 bits: weight and weight_scale as
@@ -733,15 +739,13 @@ def inner_product_int8(x, weight, weight_scale, bias=None, C=None, x_scale=None,
         _checked(dev, out, "top", top_dtype)
         if out.numel() != N * K:
             raise ValueError(f"top must have {N} x {K} elements")
-    desc = ctypes.byref(Ip8Desc(N, int(C), K, 1 if relu else 0, kind, top_kind))
-    lib, buf, buf_bytes = load(), None, 0
+    desc = Ip8Desc(N, int(C), K, 1 if relu else 0, kind, top_kind)
+    buf, buf_bytes = None, 0
     if not rows8:
-        n = ctypes.c_size_t()
-        check(lib.caffe_inner_product_int8_workspace_size(desc, ctypes.byref(n)))
-        buf = (ws or Workspace(x.device)).get(n.value)
+        buf = (ws or Workspace(x.device)).get(inner_product_int8_workspace_size(desc))
         if buf is not None:
             _checked(dev, buf, "workspace", torch.uint8)
             buf, buf_bytes = buf.data_ptr(), buf.numel()
-    _call(dev, lib.caffe_inner_product_int8, desc, x.data_ptr(), _addr(x_scale),
+    _call(dev, load().caffe_inner_product_int8, ctypes.byref(desc), x.data_ptr(), _addr(x_scale),
           weight.data_ptr(), weight_scale.data_ptr(), _addr(bias), out.data_ptr(), buf, buf_bytes)
     return out

@@ -27,8 +27,8 @@ from . import (BACKWARD_BOTTOM_STAGED, BACKWARD_BOTTOM_TERMS, BACKWARD_MASK_BOTT
                conv_uses_terms, conv_workspace_preferred, conv_workspace_size, lrn_backward, lrn_forward, maxpool_backward, maxpool_forward,
                lrn_pool_backward, pool_desc, pool_lrn_forward, pool_lrn_supported, relu_backward,
                pool_out_shape, sgd_learning_rate, sgd_update, softmax_loss,
-               inner_product_int8, muon_update, newton_schulz_workspace_size, ns_desc,
-               quantize_rows)
+               Ip8Desc, inner_product_int8, inner_product_int8_workspace_size, muon_update,
+               newton_schulz_workspace_size, ns_desc, quantize_rows)
 
 
 class ConvStack:
@@ -239,26 +239,33 @@ class ConvStack:
         # with a set of (kind, layer) keys, only those calls are marked
         self.mark_only = None
 
-    def quantize_inner_products(self):
+    def quantize_inner_products(self, stream=None):
         """Hold the weights of the inner-product layers (1x1 images) as 8-bit
         rows from now on: a quarter of the bytes (of float) that a forward pass
         reads, for scoring with a trained network.  The float weights stay; a
-        call after they changed makes the rows again.  Returns the layers'
-        indices.  A network with such layers has no backward pass."""
-        need, done = 0, []
-        for l, L in enumerate(self.layers):
-            if (L.H, L.W, L.k, L.p, L.g) != (1, 1, 1, 0, 1):
-                continue
-            q, scale = self.int8[l] or (None, None)
-            self.int8[l] = quantize_rows(self.W[l].view(L.K, L.C), q, scale)
+        call after they changed makes the rows again, in place.  Returns the
+        layers' indices.  A network with such layers has no backward pass.
+        `stream`: that of the update before and the forward passes after it."""
+        s = stream or torch.cuda.current_stream()
+        done = [l for l, L in enumerate(self.layers)
+                if (L.H, L.W, L.k, L.p, L.g) == (1, 1, 1, 0, 1)]
+        # (a layer that has no 8-bit product is refused before anything changes)
+        need = [inner_product_int8_workspace_size(
+            Ip8Desc(self.N, self.layers[l].C, self.layers[l].K, 0, CAFFE_F32, CAFFE_F32))
+            for l in done]
+        with torch.cuda.stream(s):
+            # (the same memory at every call: a captured forward pass holds it)
+            self.ws_int8.get(max(need, default=0))
+            rows = {}
+            for l in done:
+                L = self.layers[l]
+                rows[l] = quantize_rows(self.W[l].view(L.K, L.C), *(self.int8[l] or ()))
+        for l in done:
+            self.int8[l] = rows[l]
             # its input comes in float: nothing is staged for it
             self.bottom_staged[l] = False
             if l > 0:
                 self.lrn_stage_only[l - 1] = False
-            need = max(need, self.N * (self.int8[l][0].shape[1] + 4))
-            done.append(l)
-        # (the same memory at every call: a captured forward pass holds it)
-        self.ws_int8.get(need)
         return done
 
     def _mark(self, tag, s):

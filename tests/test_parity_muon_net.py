@@ -172,3 +172,54 @@ def test_rows_made_again_under_a_captured_forward():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(top, want), it
+
+
+@pytest.mark.parametrize("name", NETS)
+def test_rows_made_on_the_stream_of_the_update(name):
+    """Update, rows and scoring on one stream that is busy, nothing waited for, are
+    the same calls on the current stream."""
+    xs, ys, net = NETS[name](16)
+    _, _, one = NETS[name](16)
+    x, y = torch.from_numpy(xs[0]).to(DEV), torch.from_numpy(ys[0]).to(DEV)
+    tr, tr1 = _trainer(net), _trainer(one)
+    s = torch.cuda.Stream()
+    busy = torch.randn((2048, 2048), device=DEV)
+    ips = [l for l, L in enumerate(net.layers) if L.H == 1]
+    tr1.step(x, y)
+    want = []
+    for it in range(2):  # (the second time over the first rows)
+        assert one.quantize_inner_products() == ips
+        want.append(one.forward(x).clone())
+        for w in one.W:
+            w.mul_(-0.5)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        cc.newton_schulz(busy)
+    tr.step(x, y, stream=s)
+    for it in range(2):
+        assert net.quantize_inner_products(stream=s) == ips
+        top = net.forward(x, stream=s)
+        with torch.cuda.stream(s):
+            got = top.clone()
+            for w in net.W:
+                w.mul_(-0.5)
+            cc.newton_schulz(busy)
+        s.synchronize()
+        assert torch.equal(got, want[it]), it
+
+
+def test_a_layer_that_has_no_8_bit_rows_changes_nothing():
+    """The second layer's samples are longer than a row may be: refused, and the
+    network is as it was."""
+    C = (1 << 17) + 128
+    layers = (wl.ConvLayer("one", 32, 1, 1, C, 1, 1, 0, 1, True),
+              wl.ConvLayer("two", C, 1, 1, 3, 1, 1, 0, 1, False))
+    rng = np.random.default_rng(32)
+    W = [(rng.standard_normal((L.K, L.C, 1, 1)) * 0.05).astype(np.float32) for L in layers]
+    net = ConvStack(layers, 4, W, [np.zeros(L.K, np.float32) for L in layers])
+    x = torch.from_numpy(rng.standard_normal((4, 32, 1, 1)).astype(np.float32)).to(DEV)
+    want = net.forward(x).clone()
+    with pytest.raises(cc.CaffeError, match="C must be"):
+        net.quantize_inner_products()
+    assert net.int8 == [None, None]
+    assert torch.equal(net.forward(x), want)
