@@ -228,8 +228,12 @@ class ConvStack:
                                              p.get("pad", 0))
                 lst["lrn_desc"] = lrn_desc(pst["y"].shape, r["size"], r["alpha"], r["beta"],
                                            r["k"])
-        # (q, scale) of the layers held in 8 bits (quantize_inner_products)
+        # (q, scale) of the layers held in 8 bits (quantize_inner_products), of
+        # those that ever were, and whether the last forward pass had any
         self.int8 = [None] * n
+        self.int8_rows = [None] * n
+        self.forward_int8 = False
+        self.float_staging = list(self.bottom_staged), list(self.lrn_stage_only)
         self.ws_int8 = Workspace(dev)
         # when a list, (tag, event) pairs are recorded around every conv call:
         # tag = (kind, layer, "begin" | "end") with kind "fwd" (forward),
@@ -244,8 +248,8 @@ class ConvStack:
         rows from now on: a quarter of the bytes (of float) that a forward pass
         reads, for scoring with a trained network.  The float weights stay; a
         call after they changed makes the rows again, in place.  Returns the
-        layers' indices.  A network with such layers has no backward pass.
-        `stream`: that of the update before and the forward passes after it."""
+        layers' indices.  A network with such layers has no backward pass until
+        float_inner_products().  `stream`: that of the update before and the forward passes after it."""
         s = stream or torch.cuda.current_stream()
         done = [l for l, L in enumerate(self.layers)
                 if (L.H, L.W, L.k, L.p, L.g) == (1, 1, 1, 0, 1)]
@@ -259,13 +263,24 @@ class ConvStack:
             rows = {}
             for l in done:
                 L = self.layers[l]
-                rows[l] = quantize_rows(self.W[l].view(L.K, L.C), *(self.int8[l] or ()))
+                rows[l] = quantize_rows(self.W[l].view(L.K, L.C), *(self.int8_rows[l] or ()))
         for l in done:
-            self.int8[l] = rows[l]
+            self.int8[l] = self.int8_rows[l] = rows[l]
             # its input comes in float: nothing is staged for it
             self.bottom_staged[l] = False
             if l > 0:
                 self.lrn_stage_only[l - 1] = False
+        return done
+
+    def float_inner_products(self):
+        """Back to the float weights: forward passes as before
+        quantize_inner_products, and backward passes after the next of them.
+        Returns the indices of the layers that were held in 8 bits.  Their rows'
+        memory is kept for the next time."""
+        done = [l for l, rows in enumerate(self.int8) if rows is not None]
+        self.int8 = [None] * len(self.layers)
+        staged, stage_only = self.float_staging
+        self.bottom_staged, self.lrn_stage_only = list(staged), list(stage_only)
         return done
 
     def _mark(self, tag, s):
@@ -279,6 +294,7 @@ class ConvStack:
         s = stream or torch.cuda.current_stream()
         cur = x
         n_l = len(self.layers)
+        self.forward_int8 = any(q is not None for q in self.int8)
         for l in range(n_l):
             L = self.layers[l]
             cur = cur.view(self.N, L.C, L.H, L.W)
@@ -325,8 +341,9 @@ class ConvStack:
     def backward(self, top_diff, stream=None, data_grad_bottom=True):
         """top_diff: gradient w.r.t. the last top.  Fills dW, db and dbottom
         (dbottom[0] only when data_grad_bottom)."""
-        if any(q is not None for q in self.int8):
-            raise ValueError("layers held in 8 bits have no backward pass")
+        if self.forward_int8 or any(q is not None for q in self.int8):
+            raise ValueError("layers held in 8 bits have no backward pass: float_inner_products() "
+                             "and a forward pass come first")
         s = stream or torch.cuda.current_stream()
         # (a captured graph keeps to one stream)
         capturing = torch.cuda.is_current_stream_capturing()

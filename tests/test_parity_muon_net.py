@@ -223,3 +223,47 @@ def test_a_layer_that_has_no_8_bit_rows_changes_nothing():
         net.quantize_inner_products()
     assert net.int8 == [None, None]
     assert torch.equal(net.forward(x), want)
+
+
+def _bf16_pair(N):
+    """A fused max-pool and LRN that stage for the next convolution, and an inner product."""
+    layers = (wl.ConvLayer("conv", 3, 17, 17, 16, 3, 1, 1, 1, True),
+              wl.ConvLayer("conv2", 16, 8, 8, 32, 3, 1, 1, 1, True),
+              wl.ConvLayer("ip", 32 * 64, 1, 1, 10, 1, 1, 0, 1, False))
+    glue = {0: [("pool", dict(kernel=3, stride=2)),
+                ("lrn", dict(size=5, alpha=1e-4, beta=0.75, k=1.0))]}
+    rng = np.random.default_rng(33)
+    W = [(rng.standard_normal((L.K, L.C // L.g, L.k, L.k)) * 0.1).astype(np.float32)
+         for L in layers]
+    b = [np.zeros(L.K, np.float32) for L in layers]
+    x = rng.standard_normal((N, 3, 17, 17)).astype(np.float32)
+    return torch.from_numpy(x).to(DEV), ConvStack(layers, N, W, b, glue=glue, bf16=True)
+
+
+@pytest.mark.parametrize("name", [*NETS, "bf16"])
+def test_back_to_the_float_weights(name):
+    """Scored in 8 bits and taken back, a network gives and trains the bits of one
+    that never was; the backward pass needs a float forward pass first."""
+    if name == "bf16":
+        (x, net), (_, never) = _bf16_pair(16), _bf16_pair(16)
+    else:
+        xs, _, net = NETS[name](16)
+        never, x = NETS[name](16)[2], torch.from_numpy(xs[0]).to(DEV)
+    want = never.forward(x).clone()
+    g = torch.randn(want.shape, device=DEV)
+    never.backward(g)
+    ips = net.quantize_inner_products()
+    scores = net.forward(x).clone()
+    assert net.float_inner_products() == ips and net.float_inner_products() == []
+    with pytest.raises(ValueError, match="8 bits"):
+        net.backward(g)
+    assert net.bottom_staged == never.bottom_staged
+    assert net.lrn_stage_only == never.lrn_stage_only
+    assert torch.equal(net.forward(x), want)
+    net.backward(g)
+    torch.cuda.synchronize()
+    for a, b in zip(net.dW + net.db, never.dW + never.db):
+        assert torch.equal(a, b)
+    # and again in 8 bits, in the same rows
+    assert net.quantize_inner_products() == ips
+    assert torch.equal(net.forward(x), scores)
