@@ -23,7 +23,8 @@
  * caffe_conv.h: caller-owned 16-byte-aligned device pointers, a 256-byte
  * aligned workspace, asynchronous execution on `stream`, negative
  * caffe_status on failure with nothing enqueued, no atomics.  What a call
- * writes overlaps none of its other buffers.  Tensors may exceed 2^31 bytes.
+ * writes overlaps none of its other buffers: CAFFE_ERR_INVALID_ARG where an
+ * output overlaps an input.  Tensors may exceed 2^31 bytes.
  */
 #ifndef CAFFE_INT8_H
 #define CAFFE_INT8_H

@@ -2812,12 +2812,18 @@ static int plan_ns(const caffe_ns_desc* d, NsPlan* q)
     return CAFFE_OK;
 }
 
+// whether two buffers share memory
+static bool overlap(const void* x, uint64_t x_bytes, const void* y, uint64_t y_bytes)
+{
+    const uint64_t a = (uint64_t)x, b = (uint64_t)y;
+    return x && y && (a < b ? b - a < x_bytes : a - b < y_bytes) && x_bytes && y_bytes;
+}
+
 // whether two blobs of the batch share memory
 static bool ns_overlap(const caffe_ns_desc* d, const void* x, const void* y)
 {
     const uint64_t size = (uint64_t)d->batch * d->rows * d->cols * (d->dtype == CAFFE_BF16 ? 2 : 4);
-    const uint64_t a = (uint64_t)x, b = (uint64_t)y;
-    return (a < b ? b - a : a - b) < size;
+    return overlap(x, size, y, size);
 }
 
 static NsArgs ns_args(const caffe_ns_desc* d)
@@ -2932,6 +2938,11 @@ int caffe_quantize_rows(const void* x, int32_t dtype, int64_t rows, int32_t cols
     CHECK(check_ptr(x, rows > 0, "x"));
     CHECK(check_ptr(q, rows > 0, "q"));
     CHECK(check_ptr(scale, rows > 0, "scale"));
+    const uint64_t x_bytes = (uint64_t)rows * cols * (dtype == CAFFE_BF16 ? 2 : 4);
+    const uint64_t q_bytes = (uint64_t)rows * caffe_int8_pitch(cols), s_bytes = (uint64_t)rows * 4;
+    if (overlap(q, q_bytes, x, x_bytes) || overlap(scale, s_bytes, x, x_bytes) ||
+        overlap(q, q_bytes, scale, s_bytes))
+        return fail(CAFFE_ERR_INVALID_ARG, "q and scale must not overlap x or each other");
     LAUNCH(launch_quantize_rows(x, dtype == CAFFE_BF16, rows, cols, caffe_int8_pitch(cols), q,
                                 scale, (hipStream_t)stream),
            "row quantisation launch");
@@ -2994,6 +3005,13 @@ int caffe_inner_product_int8(const caffe_ip8_desc* desc, const void* bottom,
     CHECK(check_ptr(bias, false, "bias"));
     CHECK(check_ptr(top, nz, "top"));
     CHECK(check_ws(workspace, ws_bytes, ip8_ws(desc)));
+    const uint64_t N = desc->N, K = desc->K, pitch = caffe_int8_pitch(desc->C);
+    const uint64_t top_bytes = N * K * (desc->top_type == CAFFE_BF16 ? 2 : 4);
+    if (overlap(top, top_bytes, bottom, N * (rows8 ? pitch : (uint64_t)desc->C *
+                                             (desc->bottom_type == CAFFE_BF16 ? 2 : 4))) ||
+        overlap(top, top_bytes, bottom_scale, N * 4) || overlap(top, top_bytes, weight, K * pitch) ||
+        overlap(top, top_bytes, weight_scale, K * 4) || overlap(top, top_bytes, bias, K * 4))
+        return fail(CAFFE_ERR_INVALID_ARG, "top must not overlap the call's inputs");
     Ip8Args a{};
     a.N = desc->N;
     a.C = desc->C;

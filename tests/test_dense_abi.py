@@ -292,3 +292,44 @@ def test_workspace_keeps_what_a_graph_writes(fake_device):
     made.clear()
     gc.collect()
     assert [r().n for r in refs if r() is not None] == [20, 50, 70] and ws.buf.n == 70
+
+
+def test_8_bit_rows_that_overlap_their_input():
+    """3 x 100 floats are 1200 (0x4B0) bytes, their rows 384 (0x180), the scales 12."""
+    lib = cc.load()
+
+    def rows(x, q, s):
+        return lib.caffe_quantize_rows(P(x), 0, 3, 100, P(q), P(s), None)
+
+    far = 0x80000
+    for x, q, s in ((0x8000, 0x8000, far), (0x8000, 0x84A0, far), (0x8170, 0x8000, far),
+                    (0x8000, far, 0x8000), (0x8000, far, 0x84A0), (0x8000, far, far),
+                    (0x8000, far, far + 0x170)):
+        assert rows(x, q, s) == INVALID, (hex(x), hex(q), hex(s))
+        assert b"overlap" in lib.caffe_last_error()
+
+
+def test_top_that_overlaps_an_input():
+    """N = 3, C = 100, K = 7: 1200 bytes of bottom (384 in 8 bits, 12 of scales), 896 of
+    weights, 28 of their scales and of bias, 84 of top."""
+    lib = cc.load()
+    far = [0x100000 * i for i in range(1, 8)]
+
+    def call(bottom_type=cc.CAFFE_F32, **kw):
+        a = dict(zip(("x", "w", "t", "b", "top", "ws", "xs"), far))
+        a.update(kw)
+        if bottom_type != cc.CAFFE_INT8_ROWS:
+            a["xs"] = None
+        d = _ip8(bottom_type=bottom_type)
+        return lib.caffe_inner_product_int8(ctypes.byref(d), P(a["x"]), P(a["xs"]), P(a["w"]),
+                                            P(a["t"]), P(a["b"]), P(a["top"]), P(a["ws"]),
+                                            1 << 20, None)
+
+    top = far[4]
+    for kind, name, size in ((cc.CAFFE_F32, "x", 1200), (cc.CAFFE_BF16, "x", 600),
+                             (cc.CAFFE_INT8_ROWS, "x", 384), (cc.CAFFE_INT8_ROWS, "xs", 12),
+                             (cc.CAFFE_F32, "w", 896), (cc.CAFFE_F32, "t", 28),
+                             (cc.CAFFE_F32, "b", 28)):
+        for at in (top, top + 80, top - (size - 1) // 16 * 16):
+            assert call(kind, **{name: at}) == INVALID, (name, at - top)
+            assert b"top must not overlap" in lib.caffe_last_error()

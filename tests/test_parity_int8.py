@@ -303,3 +303,18 @@ def test_products_of_rows_with_subnormal_scales():
     w, t = cc.quantize_rows(dev(np.eye(4, dtype=np.float32) * 127))
     y = cc.inner_product_int8(dev(x), w, t)
     assert np.array_equal(y.cpu().numpy(), (q.astype(np.float32) * 127) * s[0])
+
+
+def test_buffers_next_to_each_other():
+    """Buffers without a gap between them do not overlap."""
+    x = np.random.default_rng(29).standard_normal((4, 128)).astype(np.float32)
+    buf = torch.zeros(2048 + 512 + 16 + 64, dtype=torch.uint8, device=DEV)
+    xt, q = buf[:2048].view(torch.float32).view(4, 128), buf[2048:2560].view(torch.int8).view(4, 128)
+    s, y = buf[2560:2576].view(torch.float32), buf[2576:].view(torch.float32).view(4, 4)
+    xt.copy_(dev(x))
+    check_rows(*cc.quantize_rows(xt, q=q, scale=s), x)
+    cc.inner_product_int8(q, q, s, C=128, x_scale=s, out=y)
+    assert torch.equal(y, cc.inner_product_int8(xt, q, s))
+    check_rows(q, s, x)
+    with pytest.raises(cc.CaffeError, match="overlap"):
+        cc.inner_product_int8(xt, q, s, out=xt.view(-1)[512 - 16:])
