@@ -16,8 +16,9 @@
  * weights, 8-bit, one scale t_k each):
  *   Z[n][k] = (sum_c q[n][c] p[k][c]) * s[n] * t[k] + bias[k]
  *   top[n][k] = relu ? max(Z, 0) : Z
- * The sum is exact; the scaling is in float.  With relu a NaN Z gives 0, as
- * in the convolution layer.
+ * The sum is exact for values in -127 .. 127, as rows hold them (a caller's own
+ * -128 too, up to C = 2^17 - 1); the scaling is in float.  With relu a NaN Z
+ * gives 0, as in the convolution layer.
  *
  * Conventions (memory, streams, errors, status codes) are those of
  * caffe_conv.h: caller-owned 16-byte-aligned device pointers, a 256-byte

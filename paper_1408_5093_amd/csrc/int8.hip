@@ -2,7 +2,7 @@
 // product of such rows: top[n][k] = (sum_c q[n][c] p[k][c]) s[n] t[k] + bias[k].
 //
 // The sum runs on the 8-bit matrix instructions and is exact in 32 bits
-// (C <= 2^17 and |q p| <= 2^14); only its scaling is rounded, in float.
+// (C <= 2^17, |q p| <= 127^2); only its scaling is rounded, in float.
 #include <algorithm>
 #include <type_traits>
 
@@ -20,14 +20,14 @@ typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 // rounded quotient t = fl(x / s) decides: it is on the same side of the half as
 // x / s, or on the half itself, and then the remainder x - t s says on which
 // side the quotient was.  The remainder is a multiple of half a unit of s and
-// less than 2^8 of them, exact in one fma where that half is a float: x and s
+// at most 2^8 of them, exact in one fma where that half is a float: x and s
 // below 2^-100 are taken 2^64 times.
 __device__ __forceinline__ int round_quotient(float x, float s, float inv)
 {
     const float near = x * inv;
     float r = rintf(near);
     if (!(fabsf(fabsf(near - r) - 0.5f) > 0x1p-15f)) {  // (also where inv overflows)
-        const float up = s < 0x1p-100f ? 0x1p64f : 1.f;  // exact: |x| < 2^7 s
+        const float up = s < 0x1p-100f ? 0x1p64f : 1.f;  // exact: |x| < 2^8 s
         const float xs = x * up, ss = s * up, t = xs / ss;
         r = rintf(t);
         const float d = t - r;  // exact

@@ -602,7 +602,10 @@ class MuonTrainer(SGDTrainer):
     """SGDTrainer whose weight blobs take the orthogonalised update
     (muon_update; each group of a convolution is a matrix of its own) and
     whose biases take SGD.  The weights' rate is the schedule's times
-    weight_lr / base_lr; `nesterov`, `steps` and `coef` are muon_update's."""
+    weight_lr / base_lr, their momentum weight_momentum and their decay
+    weight_decay_w, by default none: SGDTrainer's `momentum` and `weight_decay`
+    count for the biases alone here.  `nesterov`, `steps` and `coef` are
+    muon_update's."""
 
     def __init__(self, net, weight_lr=0.02, weight_momentum=0.95, weight_decay_w=0.0,
                  nesterov=True, steps=5, coef=None, **sgd):
