@@ -40,9 +40,14 @@
  * NS of a zero matrix is zero; a NaN or an infinity in U makes the whole
  * NS(U) NaN.  Its arithmetic is that of float operands: half-precision pairs
  * of 22 bits, float sums.  With the usual coefficients and 3 to 6 steps the
- * float output was within 6e-6 of its norm over 700 shapes.  With a side of at
- * most 128 that can be several times the error of steps one by one in float
- * (10 x 16: 5.1e-6, they 0.8e-6); beyond it is like theirs.
+ * float output of gradient-like matrices was within 5.3e-6 of its norm over
+ * 2900 shapes of 4 x 16 to 1500 x 1500 and 128 x 9216.  With a side of at most
+ * 128 up to half of them have over 1.5 times the error of steps one by one in
+ * float, the worst seven times (15 x 17: 5.2e-6, they 0.7e-6); with both sides
+ * longer it is like theirs.  Few dimensions with singular values near zero make
+ * more of it, five steps: 3 x 3 normal numbers up to 4.3e-5 (float steps
+ * 1.6e-6), lower triangular 2.1e-5 (1.2e-6), rank one up to 1.3e-4 at 4 x 4
+ * (3.4e-5); 40 x 40 3.7e-6 (1.1e-6), 3.9e-6 (1.0e-6), 8.7e-5 (6.4e-5).
  * The pairs hold a fixed range: an element of X_0 has an absolute error of
  * 2^-39, so parts of U more than 2^20 below ||U||_F + eps lose relative
  * accuracy; so does the result of coefficients whose steps shrink it below

@@ -424,12 +424,13 @@ hipError_t launch_inner_product_int8(const Ip8Args& a, char* ws, hipStream_t s)
         p.x = q;
         p.xs = qs;
     }
-    // The tile by the model of its time.  Measured / modelled, us:
+    // The tile by the model of its time.  Samples in 8 bits, bf16 top, measured /
+    // modelled, us:
     //        20 x 9216 x 4096  64 x 4096 x 4096  1024 x 4096 x 4096  4096 x 4096 x 4096  8192 x 9216 x 4096
-    //   32        10 / 11          7.4 / 7.1
-    //   64        15 / 19           11 / 11            35 / 34             129 / 123          521 / 535
-    //   128                         30 / 34            35 / 34              94 / 89           342 / 358
-    //   256                         57 / 84            65 / 84              86 / 84           298 / 297
+    //   32       9.6 / 11         6.8 / 7.1
+    //   64        15 / 19         8.1 / 11            30 / 34            108 / 123           466 / 535
+    //   128       45 / 62          18 / 34            29 / 34             78 / 89            298 / 358
+    //   256       83 / 160         44 / 84            51 / 84             67 / 84            259 / 297
     auto tiles = [&](int64_t side) { return (a.N + side - 1) / side * ((a.K + side - 1) / side); };
     const int64_t lines = a.pitch / 128;
     const double t32 = TileTime{3.9, 0.10, 0.18}.of(tiles(32), lines);
